@@ -180,6 +180,33 @@ FIRA_API fira_status fira_adam_dense(const fira_hparams* hp, int32_t count, void
                                      const int64_t* numel, fira_dtype dtype, int64_t t, float lr,
                                      void* cuda_stream);
 
+/* The gradients of a step together: their global norm, and clipping by it (the scheme that Section 5.4 compares the
+ * limiter with), for the lists that fira_step() and fira_adam_dense() take afterwards:
+ *   N = sqrt(sum_i ||G_i||^2);  s = max_norm / max(N, max_norm);  out_i = s G_i
+ * One tensor of the list: rows x cols, row major, ld elements from row to row (0: cols; a flat tensor is one row), of type
+ * dtype; out_ld and out_dtype say the same of out_i, which may be of the other type (fp32 sums of several micro-batches
+ * that leave as the bf16 gradients of the step).  Empty tensors are allowed, and their pointers may be NULL. */
+typedef struct {
+  int64_t rows, cols;
+  int64_t ld, out_ld;
+  int32_t dtype, out_dtype;
+} fira_grad_desc;
+
+/* G_dev: a host array of `count` device pointers, aligned to their elements (rows that start on 16-byte boundaries are
+ * the fast case).  out_dev = NULL: in place, and nothing is written where s = 1; otherwise an array like G_dev: out_i is G_i
+ * itself (same type and ld) or overlaps no tensor of the list, and no tensor is written twice.  The norm goes to
+ * norm_dev[0] and s to scale_dev[0] (device floats).  Squares are added up in double over the whole range of the
+ * types, in the same order in every call.  Where N is not finite (an infinity or a NaN among the gradients) s is 1: the
+ * gradients are passed on as they are and N tells.  max_norm > 0 (+inf: never clipped).
+ * work_dev: 16-byte aligned, fira_grad_work_bytes(count) bytes, of one call at a time; its contents need not be kept or
+ * set.  Needs no context.  Asynchronous on cuda_stream. */
+FIRA_API size_t fira_grad_work_bytes(int32_t count);
+FIRA_API fira_status fira_grad_norm(int32_t count, const fira_grad_desc* descs, const void* const* G_dev,
+                                    float* norm_dev, void* work_dev, size_t work_bytes, void* cuda_stream);
+FIRA_API fira_status fira_clip_grads(int32_t count, const fira_grad_desc* descs, const void* const* G_dev,
+                                     void* const* out_dev, float max_norm, float* norm_dev, float* scale_dev,
+                                     void* work_dev, size_t work_bytes, void* cuda_stream);
+
 /* The same pass as fira_step() (Algorithm 1's loop body) for callers whose weights
  * and gradients live in HOST memory: W_host and G_host are host arrays of `count`
  * host pointers (m x ld elements each; page-locked memory makes the copies

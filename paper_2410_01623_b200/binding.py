@@ -7,6 +7,7 @@ library is missing, `lib()` raises; there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional, Sequence, Tuple
@@ -42,6 +43,11 @@ class MatrixDesc(C.Structure):
 class Diag(C.Structure):
     _fields_ = [("norm_scaled", C.c_float), ("lambda_", C.c_float), ("norm_prev", C.c_float),
                 ("k_min", C.c_float), ("k_max", C.c_float), ("t", C.c_int64), ("engine", C.c_int32)]
+
+
+class GradDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64), ("out_ld", C.c_int64),
+                ("dtype", C.c_int32), ("out_dtype", C.c_int32)]
 
 
 class FiraError(RuntimeError):
@@ -90,6 +96,11 @@ SIGNATURES = {
     "fira_adam_dense": (C.c_int, [C.POINTER(Hparams), C.c_int32, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
                                   C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.POINTER(C.c_int64), C.c_int,
                                   C.c_int64, C.c_float, C.c_void_p]),
+    "fira_grad_work_bytes": (C.c_size_t, [C.c_int32]),
+    "fira_grad_norm": (C.c_int, [C.c_int32, C.POINTER(GradDesc), C.POINTER(C.c_void_p), C.c_void_p, C.c_void_p,
+                                 C.c_size_t, C.c_void_p]),
+    "fira_clip_grads": (C.c_int, [C.c_int32, C.POINTER(GradDesc), C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
+                                  C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "fira_status_string": (C.c_char_p, [C.c_int]),
     "fira_last_error": (C.c_char_p, []),
     "fira_destroy": (None, [C.c_void_p]),
@@ -148,6 +159,113 @@ def adam_dense(hp: Hparams, Ws: Sequence[torch.Tensor], Gs: Sequence[torch.Tenso
         check(lib().fira_adam_dense(C.byref(hp), n, ptr_array(Ws), ptr_array(Gs), ptr_array(Ms), ptr_array(Vs),
                                     numel, 1 if dt == torch.bfloat16 else 0, int(t),
                                     -1.0 if lr is None else float(lr), C.c_void_p(stream)))
+
+
+_CODES = {torch.float32: FIRA_F32, torch.bfloat16: FIRA_BF16}
+
+
+def _code(t: torch.Tensor, what: str) -> int:
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{what}: float32 or bfloat16, not {t.dtype}")
+    return code
+
+
+@contextlib.contextmanager
+def _other_device(device):
+    with torch.cuda.device(device):
+        yield
+
+
+def _on(device: torch.device):
+    """The device whose tensors a call gets, as the current one (torch.cuda.device costs a few microseconds, which a
+    call on the current device need not pay)."""
+    if device.type != "cuda":
+        raise ValueError(f"the Fira library runs on a CUDA device only, not on {device}")
+    return _HERE if device.index == torch.cuda.current_device() else _other_device(device)
+
+
+_HERE = contextlib.nullcontext()
+
+
+def _rows(t: torch.Tensor, flip: bool):
+    """(rows, cols, ld) of a 2-D tensor, or of its transpose, as a row-major matrix; None if it is none."""
+    if t.dim() != 2:
+        return None
+    (m, n), (a, b) = (t.shape, t.stride()) if not flip else (t.shape[::-1], t.stride()[::-1])
+    if (n > 1 and b != 1) or (m > 1 and a < n):
+        return None
+    return m, n, (a if m > 1 else n)
+
+
+def _grad_list(Gs: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]]):
+    """The descriptors and pointers of a list of gradients."""
+    n = len(Gs)
+    if n == 0:
+        raise ValueError("an empty list of gradients")
+    device = Gs[0].device
+    words, ptrs, out_ptrs = [], [], []
+    for i, g in enumerate(Gs):
+        o = g if out is None else out[i]
+        if g.device != device or o.device != device or o.shape != g.shape:
+            raise ValueError(f"gradient {i}: {tuple(g.shape)} on {g.device}, its output {tuple(o.shape)} on {o.device}, "
+                             f"the first gradient on {device}")
+        code, out_code = _CODES.get(g.dtype), _CODES.get(o.dtype)
+        if code is None or out_code is None:
+            raise ValueError(f"gradient {i}: float32 or bfloat16, not {g.dtype if code is None else o.dtype}")
+        if g.is_contiguous() and o.is_contiguous():
+            words += (1, g.numel(), 0, 0, code | out_code << 32)
+        else:
+            for flip in (False, True):         # a matrix and its transpose have the same elements, in another order
+                a, b = _rows(g, flip), _rows(o, flip)
+                if a is not None and b is not None:
+                    words += (*a, b[2], code | out_code << 32)
+                    break
+            else:
+                raise ValueError(f"gradient {i}: strides {tuple(g.stride())} and, of its output, {tuple(o.stride())} "
+                                 f"of shape {tuple(g.shape)}: not both row-major, or both transposed, matrices")
+        ptrs.append(g.data_ptr())
+        out_ptrs.append(o.data_ptr())
+    table = (C.c_int64 * (5 * n))(*words)
+    return (device, n, C.cast(table, C.POINTER(GradDesc)), (C.c_void_p * n)(*ptrs),
+            None if out is None else (C.c_void_p * n)(*out_ptrs))
+
+
+def grad_norm(Gs: Sequence[torch.Tensor], work: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """fira_grad_norm: the norm over all elements of a list of gradients (float32 and bfloat16 may be mixed), as a
+    float32 tensor of one element on the device; nothing waits for it.  work: a byte tensor of at least
+    grad_work_bytes(len(Gs)) bytes; by default torch's allocator lends one for the call."""
+    device, n, descs, ptrs, _ = _grad_list(Gs, None)
+    with _on(device):
+        nbytes = lib().fira_grad_work_bytes(n)
+        if work is None:
+            work = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        norm = torch.empty((), dtype=torch.float32, device=device)
+        check(lib().fira_grad_norm(n, descs, ptrs, norm.data_ptr(), work.data_ptr(), work.numel() * work.element_size(),
+                                   torch.cuda.current_stream().cuda_stream))
+    return norm
+
+
+def clip_grads(Gs: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None,
+               work: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """fira_clip_grads: scales a list of gradients so that their global norm is at most max_norm, in place or into `out`
+    (tensors of the same shapes, float32 or bfloat16 each), and returns the norm before it and the factor, as float32
+    tensors of one element on the device."""
+    if out is not None and len(out) != len(Gs):
+        raise ValueError(f"{len(out)} outputs for {len(Gs)} gradients")
+    device, n, descs, ptrs, out_ptrs = _grad_list(Gs, out)
+    with _on(device):
+        if work is None:
+            work = torch.empty(lib().fira_grad_work_bytes(n), dtype=torch.uint8, device=device)
+        both = torch.empty(2, dtype=torch.float32, device=device)
+        at = both.data_ptr()
+        check(lib().fira_clip_grads(n, descs, ptrs, out_ptrs, max_norm, at, at + 4, work.data_ptr(),
+                                    work.numel() * work.element_size(), torch.cuda.current_stream().cuda_stream))
+    return both[0], both[1]
+
+
+def grad_work_bytes(count: int) -> int:
+    return lib().fira_grad_work_bytes(count)
 
 
 class Fira:

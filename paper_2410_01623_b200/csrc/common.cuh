@@ -134,6 +134,12 @@ __device__ __forceinline__ int find_matrix(const int* __restrict__ start, int co
 
 void set_error(const std::string& msg);
 
+// The body of an entry point that builds messages and lists: nothing is thrown across the C boundary.
+template <typename F>
+inline fira_status guarded(F&& body) noexcept {
+  try { return body(); } catch (...) { return FIRA_ERR_UNSUPPORTED; }   // out of host memory
+}
+
 // Launches a kernel in clusters of `cluster` blocks (1: none, or the kernel's own).  chained: every block of the kernel
 // calls ptx::grid_wait, and its blocks may start while the kernel in front of it in the stream is still running: between
 // two short kernels that saves 3 to 5 us.

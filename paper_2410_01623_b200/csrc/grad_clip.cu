@@ -1,0 +1,405 @@
+// The norm over a list of gradients, and clipping by it.
+//
+//   N = sqrt(sum_i ||G_i||^2),  s = max_norm / max(N, max_norm),  out_i = s G_i
+//
+// Two kernels over a list of tensors whose table travels in the kernel arguments (nothing is allocated, nothing of
+// it outlives the call).  k_grad_squares leaves one sum of squares per block; k_grad_scale adds those up in a fixed
+// order in every block (they are a few KB), so that no third launch lies between, and scales.  Sums are the same in
+// every call: no atomics.
+//
+// A thread squares 32 elements into one fp32 sum and adds that to a double.  Where the fp32 sum says nothing (it left
+// the range in which neither an overflow nor what underflowed matters) the elements, still in registers, are squared
+// again in double: the norm holds over the whole range of the types.
+#include <math.h>
+
+#include <algorithm>
+
+#include "common.cuh"
+#include "tc_ptx.cuh"
+
+namespace fira {
+namespace {
+
+constexpr int GC_THREADS = 256;
+constexpr int GC_CHUNK = 8;                       // elements of a chunk: 16 bytes of bf16, 32 of fp32
+constexpr int GC_UNROLL = 4;                      // chunks of a thread in flight
+constexpr int GC_TILE = GC_THREADS * GC_UNROLL;   // chunks of a tile (8192 elements)
+constexpr int GC_SMS = 148;
+constexpr int GC_BLOCKS = GC_SMS * 4;             // blocks of a launch: tiles are dealt to them in turn
+constexpr int GC_MANY = 512, GC_FEW = 48;         // tensors of a launch: 28 KB of kernel arguments, or 2.7 KB
+
+// One tensor.  A flat one is one row; rows of a pitched one start on their own.
+struct GradEntry {
+  const void* g;
+  void* o;
+  long long ld, out_ld;     // of a pitched tensor, elements
+  long long n;              // elements of a row
+  long long chunks;         // of the whole tensor
+  int tile_start;           // tiles of the tensors in front of it
+  unsigned char bf16, out_bf16;
+  unsigned char single;     // a chunk is one element: rows that do not start on 16-byte boundaries
+  unsigned char pitched;
+};
+
+template <int CAP>
+struct GradTable {
+  GradEntry t[CAP];
+  int count, tiles;
+};
+
+__device__ __forceinline__ void unpack8(const uint4& u, float (&v)[8]) {
+  const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+
+// Where chunk c of the tensor starts in G and in out, and how many elements it has.
+struct Place { long long at, out_at; int len; };
+__device__ __forceinline__ Place place(const GradEntry& t, long long c, long long row0, unsigned col0, unsigned local) {
+  const int w = t.single ? 1 : GC_CHUNK;
+  Place p;
+  if (!t.pitched) {
+    p.at = p.out_at = c * w;
+    const long long left = t.n - p.at;
+    p.len = left < w ? (int)left : w;
+  } else {
+    const unsigned per_row = (unsigned)((t.n + w - 1) / w);
+    const unsigned x = col0 + local, down = x / per_row;      // col0 < per_row < 2^31, local < 2^11: no overflow
+    const long long col = (long long)(x - down * per_row) * w;
+    p.at = (row0 + down) * t.ld + col;
+    p.out_at = (row0 + down) * t.out_ld + col;
+    const long long left = t.n - col;
+    p.len = left < w ? (int)left : w;
+  }
+  return p;
+}
+
+__device__ __forceinline__ void load_chunk(const GradEntry& t, const Place& p, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = 0.f;
+  if (p.len == 8) {
+    if (t.bf16) {
+      unpack8(*reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(t.g) + p.at), v);
+    } else {
+      const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(t.g) + p.at);
+      const float4 a = q[0], b = q[1];
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < p.len) v[e] = t.bf16 ? to_float(static_cast<const __nv_bfloat16*>(t.g)[p.at + e]) : static_cast<const float*>(t.g)[p.at + e];
+  }
+}
+
+__device__ __forceinline__ void store_chunk(const GradEntry& t, const Place& p, const float (&v)[8]) {
+  if (p.len == 8) {
+    if (t.out_bf16) {
+      uint4 u;
+      unsigned* w = reinterpret_cast<unsigned*>(&u);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const unsigned*>(&h);
+      }
+      *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(t.o) + p.out_at) = u;
+    } else {
+      float4* q = reinterpret_cast<float4*>(static_cast<float*>(t.o) + p.out_at);
+      q[0] = make_float4(v[0], v[1], v[2], v[3]);
+      q[1] = make_float4(v[4], v[5], v[6], v[7]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < p.len) {
+        if (t.out_bf16) static_cast<__nv_bfloat16*>(t.o)[p.out_at + e] = __float2bfloat16_rn(v[e]);
+        else static_cast<float*>(t.o)[p.out_at + e] = v[e];
+      }
+  }
+}
+
+// The chunks of this thread in a tile.
+struct Tile {
+  int q;                       // tensor
+  long long first, row0;       // first chunk; for a pitched tensor its row and column
+  unsigned col0;
+};
+__device__ __forceinline__ Tile open_tile(const GradEntry* t, int q, int tile) {
+  Tile x;
+  x.q = q;
+  x.first = (long long)(tile - t[q].tile_start) * GC_TILE;
+  x.row0 = 0; x.col0 = 0;
+  if (t[q].pitched) {
+    const int w = t[q].single ? 1 : GC_CHUNK;
+    const long long per_row = (t[q].n + w - 1) / w;
+    x.row0 = x.first / per_row;
+    x.col0 = (unsigned)(x.first - x.row0 * per_row);
+  }
+  return x;
+}
+
+__device__ __forceinline__ void load_tile(const GradEntry* tab, const Tile& x, Place (&p)[GC_UNROLL], float (&v)[GC_UNROLL][8]) {
+  const GradEntry& t = tab[x.q];
+#pragma unroll
+  for (int u = 0; u < GC_UNROLL; ++u) {
+    const unsigned local = u * GC_THREADS + threadIdx.x;
+    const long long c = x.first + local;
+    if (c < t.chunks) {
+      p[u] = place(t, c, x.row0, x.col0, local);
+    } else {
+      p[u].at = p[u].out_at = 0; p[u].len = 0;
+    }
+    load_chunk(t, p[u], v[u]);
+  }
+}
+
+__device__ __forceinline__ double block_sum(double s, double* smem) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if ((threadIdx.x & 31) == 0) smem[threadIdx.x >> 5] = s;
+  __syncthreads();
+  double r = 0.0;
+#pragma unroll
+  for (int w = 0; w < GC_THREADS / 32; ++w) r += smem[w];
+  return r;
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(GC_THREADS, 4)
+k_grad_squares(const __grid_constant__ GradTable<CAP> tab, double* __restrict__ sums) {
+  __shared__ double red[GC_THREADS / 32];
+  ptx::grid_launch_next();     // its blocks take the places that ours leave, and wait for the last of ours
+  double total = 0.0;
+  int q = 0;
+  for (int tile = blockIdx.x; tile < tab.tiles; tile += gridDim.x) {
+    while (q + 1 < tab.count && tile >= tab.t[q + 1].tile_start) ++q;
+    Place p[GC_UNROLL];
+    float v[GC_UNROLL][8];
+    load_tile(tab.t, open_tile(tab.t, q, tile), p, v);
+    float s = 0.f;
+#pragma unroll
+    for (int u = 0; u < GC_UNROLL; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fmaf(v[u][e], v[u][e], s);
+    if (s >= 0x1p-80f && s <= 0x1p126f) {
+      total += (double)s;      // what underflowed is below 32 * 2^-126, the rounding below 32 * 2^-24 of s
+    } else {
+      bool any = false;
+#pragma unroll
+      for (int u = 0; u < GC_UNROLL; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) any |= v[u][e] != 0.f;
+      if (any) {
+        double d = 0.0;
+#pragma unroll
+        for (int u = 0; u < GC_UNROLL; ++u)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) d = fma((double)v[u][e], (double)v[u][e], d);
+        total += d;
+      }
+    }
+  }
+  const double r = block_sum(total, red);
+  if (threadIdx.x == 0) sums[blockIdx.x] = r;
+}
+
+// The norm from the sums of all blocks, in an order that their number alone fixes.
+__device__ __forceinline__ double norm_of(const double* sums, int nsums, double* red) {
+  double s = 0.0;
+  for (int i = threadIdx.x; i < nsums; i += GC_THREADS) s += sums[i];
+  return sqrt(block_sum(s, red));
+}
+
+__global__ void __launch_bounds__(GC_THREADS)
+k_grad_norm(const double* __restrict__ sums, int nsums, float* norm_out) {
+  __shared__ double red[GC_THREADS / 32];
+  ptx::grid_wait();
+  const double norm = norm_of(sums, nsums, red);
+  if (threadIdx.x == 0) *norm_out = (float)norm;
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(GC_THREADS, 4)
+k_grad_scale(const __grid_constant__ GradTable<CAP> tab, const double* __restrict__ sums, int nsums, float max_norm,
+             float* norm_out, float* scale_out, int in_place) {
+  __shared__ double red[GC_THREADS / 32];
+  ptx::grid_wait();
+  const double norm = norm_of(sums, nsums, red);
+  const bool finite = norm <= 1.7976931348623157e308;
+  const float scale = finite && norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.f;
+  if (blockIdx.x == 0 && threadIdx.x == 0) { *norm_out = (float)norm; *scale_out = scale; }
+  if (in_place && scale == 1.f) return;
+  int q = tab.count - 1;
+  // from the end: what the sums read last is what the L2 still holds
+  for (int tile = tab.tiles - 1 - (int)blockIdx.x; tile >= 0; tile -= gridDim.x) {
+    while (tile < tab.t[q].tile_start) --q;
+    Place p[GC_UNROLL];
+    float v[GC_UNROLL][8];
+    load_tile(tab.t, open_tile(tab.t, q, tile), p, v);
+#pragma unroll
+    for (int u = 0; u < GC_UNROLL; ++u) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[u][e] *= scale;
+      if (p[u].len) store_chunk(tab.t[q], p[u], v[u]);
+    }
+  }
+}
+
+int launches_for(int count) { return (count + GC_MANY - 1) / GC_MANY; }
+
+fira_status check_list(const char* who, int32_t count, const fira_grad_desc* descs, const void* const* G_dev, void* const* out_dev) {
+  const std::string name(who);
+  if (count <= 0 || !descs || !G_dev) { set_error(name + ": null argument or empty list"); return FIRA_ERR_INVALID_ARG; }
+  for (int base = 0; base < count; base += GC_MANY) {
+    long long tiles = 0;
+    for (int i = base; i < std::min(count, base + GC_MANY); ++i) {
+      const fira_grad_desc& d = descs[i];
+      const std::string at = name + ": tensor " + std::to_string(i) + ": ";
+      if (d.rows < 0 || d.cols < 0) { set_error(at + "negative size"); return FIRA_ERR_INVALID_ARG; }
+      if (d.rows > 1 && ((d.ld != 0 && d.ld < d.cols) || (out_dev && d.out_ld != 0 && d.out_ld < d.cols))) {
+        set_error(at + "ld below the width"); return FIRA_ERR_INVALID_ARG;
+      }
+      if ((d.dtype != FIRA_F32 && d.dtype != FIRA_BF16) || (out_dev && d.out_dtype != FIRA_F32 && d.out_dtype != FIRA_BF16)) {
+        set_error(at + "unknown dtype"); return FIRA_ERR_INVALID_ARG;
+      }
+      if (d.rows == 0 || d.cols == 0) continue;
+      if (d.rows > (1ll << 40) || d.cols > (1ll << 40) || d.rows > (1ll << 42) / d.cols || (d.rows > 1 && (d.cols >= (1ll << 31) - GC_TILE || d.ld > (1ll << 40) || d.out_ld > (1ll << 40)))) {
+        set_error(at + "too large"); return FIRA_ERR_INVALID_ARG;
+      }
+      const size_t es = d.dtype == FIRA_BF16 ? 2 : 4, os = d.out_dtype == FIRA_BF16 ? 2 : 4;
+      if (!G_dev[i] || ((uintptr_t)G_dev[i] & (es - 1)) || (out_dev && (!out_dev[i] || ((uintptr_t)out_dev[i] & (os - 1))))) {
+        set_error(at + "pointers must be non-null and aligned to their elements"); return FIRA_ERR_INVALID_ARG;
+      }
+      // every element a chunk of its own is the most that a tensor takes
+      tiles += (d.rows * d.cols + GC_TILE - 1) / GC_TILE;
+    }
+    if (tiles > 0x7fff0000ll) { set_error(name + ": too many elements in one call"); return FIRA_ERR_INVALID_ARG; }
+  }
+  return FIRA_OK;
+}
+
+// No tensor may be written twice, and one written over its own input keeps its type and layout.
+fira_status check_outputs(int32_t count, const fira_grad_desc* descs, const void* const* G_dev, void* const* out_dev) {
+  if (count <= 0 || !descs || !G_dev) return FIRA_OK;      // said by check_list
+  std::vector<const void*> written;
+  written.reserve(count);
+  for (int i = 0; i < count; ++i) {
+    const fira_grad_desc& d = descs[i];
+    if (d.rows <= 0 || d.cols <= 0) continue;
+    if (out_dev && out_dev[i] == G_dev[i] && (d.dtype != d.out_dtype || (d.rows > 1 && (d.ld ? d.ld : d.cols) != (d.out_ld ? d.out_ld : d.cols)))) {
+      set_error("fira_clip_grads: tensor " + std::to_string(i) + ": in place needs the same type and ld"); return FIRA_ERR_INVALID_ARG;
+    }
+    written.push_back(out_dev ? out_dev[i] : G_dev[i]);
+  }
+  std::sort(written.begin(), written.end());
+  if (std::adjacent_find(written.begin(), written.end()) != written.end()) {
+    set_error("fira_clip_grads: a tensor is written twice"); return FIRA_ERR_INVALID_ARG;
+  }
+  return FIRA_OK;
+}
+
+template <int CAP>
+void fill(GradTable<CAP>& tab, int base, int n, const fira_grad_desc* descs, const void* const* G_dev, void* const* out_dev) {
+  long long tiles = 0;
+  tab.count = 0;
+  for (int i = base; i < base + n; ++i) {
+    const fira_grad_desc& d = descs[i];
+    if (d.rows == 0 || d.cols == 0) continue;
+    const long long ld = d.rows == 1 || d.ld == 0 ? d.cols : d.ld;
+    const long long out_ld = !out_dev ? ld : d.rows == 1 || d.out_ld == 0 ? d.cols : d.out_ld;
+    const size_t es = d.dtype == FIRA_BF16 ? 2 : 4;
+    GradEntry& t = tab.t[tab.count++];
+    t.g = G_dev[i];
+    t.o = out_dev ? out_dev[i] : const_cast<void*>(G_dev[i]);
+    t.bf16 = d.dtype == FIRA_BF16;
+    t.out_bf16 = out_dev ? d.out_dtype == FIRA_BF16 : t.bf16;
+    const size_t os = t.out_bf16 ? 2 : 4;
+    t.ld = ld; t.out_ld = out_ld;
+    t.pitched = ld != d.cols || out_ld != d.cols;
+    t.n = t.pitched ? d.cols : d.rows * d.cols;
+    t.single = (((uintptr_t)t.g | (uintptr_t)t.o) & 15) != 0 || (t.pitched && ((ld * es | out_ld * os) & 15) != 0);
+    const long long w = t.single ? 1 : GC_CHUNK;
+    t.chunks = (t.pitched ? d.rows : 1) * ((t.n + w - 1) / w);
+    t.tile_start = (int)tiles;
+    tiles += (t.chunks + GC_TILE - 1) / GC_TILE;
+  }
+  tab.tiles = (int)tiles;
+}
+
+// out_dev null: in place.  scale_dev null: the norm alone.
+template <int CAP>
+cudaError_t run_list(int32_t count, const fira_grad_desc* descs, const void* const* G_dev, void* const* out_dev, float max_norm,
+                     float* norm_dev, float* scale_dev, double* sums, cudaStream_t st) {
+  GradTable<CAP> tab;
+  int nsums = 0;
+  for (int base = 0; base < count; base += CAP) {
+    fill(tab, base, std::min(CAP, count - base), descs, G_dev, out_dev);
+    const int blocks = std::max(1, std::min(GC_BLOCKS, tab.tiles));
+    k_grad_squares<CAP><<<blocks, GC_THREADS, 0, st>>>(tab, sums + nsums);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    nsums += blocks;
+  }
+  if (!scale_dev) return launch_chained(k_grad_norm, dim3(1), GC_THREADS, 0, st, true, 1, (const double*)sums, nsums, norm_dev);
+  bool chained = true;          // only behind the sums: a second part of a long list runs behind a kernel that lets it in at its end
+  for (int base = (count - 1) / CAP * CAP; base >= 0; base -= CAP) {
+    if (count > CAP) fill(tab, base, std::min(CAP, count - base), descs, G_dev, out_dev);
+    const int blocks = std::max(1, std::min(GC_BLOCKS, tab.tiles));
+    const cudaError_t e = launch_chained(k_grad_scale<CAP>, dim3(blocks), GC_THREADS, 0, st, chained, 1, tab, (const double*)sums, nsums,
+                                         max_norm, norm_dev, scale_dev, out_dev == nullptr ? 1 : 0);
+    if (e != cudaSuccess) return e;
+    chained = false;
+  }
+  return cudaSuccess;
+}
+
+fira_status run(const char* who, int32_t count, const fira_grad_desc* descs, const void* const* G_dev, void* const* out_dev, float max_norm,
+                float* norm_dev, float* scale_dev, void* work_dev, size_t work_bytes, void* cuda_stream) {
+  const fira_status bad = check_list(who, count, descs, G_dev, out_dev);
+  if (bad != FIRA_OK) return bad;
+  if (!norm_dev || !work_dev || ((uintptr_t)work_dev & 15) || ((uintptr_t)norm_dev & 3) || ((uintptr_t)scale_dev & 3)) {
+    set_error(std::string(who) + ": norm, scale and work must be aligned device pointers (work: 16 bytes)"); return FIRA_ERR_INVALID_ARG;
+  }
+  if (work_bytes < fira_grad_work_bytes(count)) {
+    set_error(std::string(who) + ": workspace too small: " + std::to_string(work_bytes) + " bytes, " + std::to_string(fira_grad_work_bytes(count)) + " needed");
+    return FIRA_ERR_WORKSPACE_TOO_SMALL;
+  }
+  double* sums = static_cast<double*>(work_dev);
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  const cudaError_t e = count <= GC_FEW ? run_list<GC_FEW>(count, descs, G_dev, out_dev, max_norm, norm_dev, scale_dev, sums, st)
+                                        : run_list<GC_MANY>(count, descs, G_dev, out_dev, max_norm, norm_dev, scale_dev, sums, st);
+  if (e != cudaSuccess) { set_error(std::string(who) + ": " + cudaGetErrorString(e)); return FIRA_ERR_CUDA; }
+  return FIRA_OK;
+}
+
+}  // namespace
+}  // namespace fira
+
+using namespace fira;
+
+extern "C" size_t fira_grad_work_bytes(int32_t count) {
+  return (size_t)std::max(1, launches_for(std::max(1, count))) * GC_BLOCKS * sizeof(double);
+}
+
+extern "C" fira_status fira_grad_norm(int32_t count, const fira_grad_desc* descs, const void* const* G_dev, float* norm_dev,
+                                      void* work_dev, size_t work_bytes, void* cuda_stream) {
+  return guarded([&] {
+    return run("fira_grad_norm", count, descs, G_dev, nullptr, 1.f, norm_dev, nullptr, work_dev, work_bytes, cuda_stream);
+  });
+}
+
+extern "C" fira_status fira_clip_grads(int32_t count, const fira_grad_desc* descs, const void* const* G_dev, void* const* out_dev,
+                                       float max_norm, float* norm_dev, float* scale_dev, void* work_dev, size_t work_bytes,
+                                       void* cuda_stream) {
+  return guarded([&]() -> fira_status {
+    if (!(max_norm > 0.f)) { set_error("fira_clip_grads: max_norm must be > 0"); return FIRA_ERR_INVALID_ARG; }
+    if (!scale_dev) { set_error("fira_clip_grads: null argument or empty list"); return FIRA_ERR_INVALID_ARG; }
+    const fira_status bad = check_outputs(count, descs, G_dev, out_dev);
+    if (bad != FIRA_OK) return bad;
+    return run("fira_clip_grads", count, descs, G_dev, out_dev, max_norm, norm_dev, scale_dev, work_dev, work_bytes, cuda_stream);
+  });
+}
