@@ -207,6 +207,28 @@ FIRA_API fira_status fira_clip_grads(int32_t count, const fira_grad_desc* descs,
                                      void* const* out_dev, float max_norm, float* norm_dev, float* scale_dev,
                                      void* work_dev, size_t work_bytes, void* cuda_stream);
 
+/* The embedding table, one of the parameters that fira_adam_dense() steps: its rows for a batch of tokens, and its gradient.
+ *   Y_i = scale E[t_i];    G_v = scale sum over {i : t_i = v} of dY_i
+ * Tokens are 32- or 64-bit integers (token_bits) at addresses aligned to them, `count` in all; a position whose token is not
+ * in 0 .. vocab-1 (-1 behind the end of a sequence) gives a row of zeros and has no part in the gradient.  Rows have
+ * `hidden` elements and are ld (ld_out, ldg) elements apart (0: hidden); tensors are aligned to their elements, and rows of
+ * whole 16-byte units that start on 16-byte boundaries are the fast case.  Products and sums are fp32 and rounded once; the
+ * order of a sum depends on the tokens alone, so the same call gives the same bits.
+ * Lookup: table and out have type dtype; out must not overlap the table.
+ * Gradient: dY has type dtype, G (vocab rows) type grad_dtype.  accumulate = 0: all of G is written, rows without a token
+ * as zeros.  accumulate != 0: the sums are added to what is there (micro-batches; a table that is also the output head),
+ * and rows without a token are left alone.  work_dev: 256-byte aligned, fira_embedding_grad_work_bytes() bytes of the same
+ * sizes (0: sizes that the call refuses), of one call at a time; its contents need not be kept or set.
+ * count = 0 is allowed.  Need no context.  Asynchronous on cuda_stream. */
+FIRA_API fira_status fira_embedding(const void* table_dev, int64_t vocab, int64_t hidden, int64_t ld, fira_dtype dtype,
+                                    const void* tokens_dev, int32_t token_bits, int64_t count, float scale,
+                                    void* out_dev, int64_t ld_out, void* cuda_stream);
+FIRA_API size_t fira_embedding_grad_work_bytes(int64_t count, int64_t vocab, int64_t hidden, fira_dtype dtype);
+FIRA_API fira_status fira_embedding_grad(const void* tokens_dev, int32_t token_bits, int64_t count, const void* dY_dev,
+                                         int64_t ld, fira_dtype dtype, int64_t vocab, int64_t hidden, float scale,
+                                         void* G_dev, int64_t ldg, fira_dtype grad_dtype, int32_t accumulate,
+                                         void* work_dev, size_t work_bytes, void* cuda_stream);
+
 /* The same pass as fira_step() (Algorithm 1's loop body) for callers whose weights
  * and gradients live in HOST memory: W_host and G_host are host arrays of `count`
  * host pointers (m x ld elements each; page-locked memory makes the copies

@@ -215,7 +215,7 @@ __device__ __forceinline__ double norm_of(const double* sums, int nsums, double*
 }
 
 __global__ void __launch_bounds__(GC_THREADS)
-k_grad_norm(const double* __restrict__ sums, int nsums, float* norm_out) {
+k_grad_norm(const double* sums, int nsums, float* norm_out) {
   __shared__ double red[GC_THREADS / 32];
   ptx::grid_wait();
   const double norm = norm_of(sums, nsums, red);
@@ -224,7 +224,7 @@ k_grad_norm(const double* __restrict__ sums, int nsums, float* norm_out) {
 
 template <int CAP>
 __global__ void __launch_bounds__(GC_THREADS, 4)
-k_grad_scale(const __grid_constant__ GradTable<CAP> tab, const double* __restrict__ sums, int nsums, float max_norm,
+k_grad_scale(const __grid_constant__ GradTable<CAP> tab, const double* sums, int nsums, float max_norm,
              float* norm_out, float* scale_out, int in_place) {
   __shared__ double red[GC_THREADS / 32];
   ptx::grid_wait();
