@@ -229,6 +229,32 @@ FIRA_API fira_status fira_embedding_grad(const void* tokens_dev, int32_t token_b
                                          void* G_dev, int64_t ldg, fira_dtype grad_dtype, int32_t accumulate,
                                          void* work_dev, size_t work_bytes, void* cuda_stream);
 
+/* Layer norm over rows of `hidden` elements (at most 16384; more: FIRA_ERR_UNSUPPORTED), whose gains (and biases) are
+ * parameters that fira_adam_dense() steps, and its backward pass.  Without mean (mean_dev = NULL) it is the RMS form, which
+ * has no bias:
+ *   mu = mean(x) (RMS: 0);  s = 1 / sqrt(mean((x - mu)^2) + eps);  y = (x - mu) s gain + bias
+ *   with h = (x - mu) s, q = dY gain:  dX = s (q - mean(q) - h mean(q h))   (RMS: without mean(q))
+ *   dgain = sum over rows of dY h;  dbias = sum over rows of dY
+ * x, y, dY, dX have type dtype and rows ld elements apart (0: hidden); gain and bias type param_dtype; dgain and dbias type
+ * grad_dtype.  bias_dev may be NULL (none), dbias_dev too (not wanted).  Tensors are aligned to their elements; rows of whole 16-byte units that
+ * start on 16-byte boundaries are the fast case.  The forward pass writes rstd_dev[row] = s and mean_dev[row] = mu, which
+ * the backward pass takes.  Arithmetic and sums are fp32, rounded once; the sums over rows are made in the same order in
+ * every call.  accumulate != 0: dgain and dbias are added to what is there.
+ * y may be x itself, dX may be dY or x itself (same ld); otherwise they overlap nothing.  nrows = 0 is allowed (dgain and dbias
+ * are then zero, or left as they are).  work_dev: 256-byte aligned, fira_layer_norm_grad_work_bytes() bytes of the same
+ * sizes (0: sizes that the call refuses), of one call at a time; its contents need not be kept or set.  Need no context.
+ * Asynchronous on cuda_stream. */
+FIRA_API fira_status fira_layer_norm(const void* x_dev, int64_t ld_x, fira_dtype dtype, int64_t nrows, int64_t hidden,
+                                     const void* gain_dev, const void* bias_dev, fira_dtype param_dtype, float eps,
+                                     void* y_dev, int64_t ld_y, float* mean_dev, float* rstd_dev, void* cuda_stream);
+FIRA_API size_t fira_layer_norm_grad_work_bytes(int64_t nrows, int64_t hidden, fira_dtype dtype);
+FIRA_API fira_status fira_layer_norm_grad(const void* dY_dev, int64_t ld_dy, const void* x_dev, int64_t ld_x,
+                                          fira_dtype dtype, int64_t nrows, int64_t hidden, const void* gain_dev,
+                                          fira_dtype param_dtype, const float* mean_dev, const float* rstd_dev,
+                                          void* dX_dev, int64_t ld_dx, void* dgain_dev, void* dbias_dev,
+                                          fira_dtype grad_dtype, int32_t accumulate, void* work_dev, size_t work_bytes,
+                                          void* cuda_stream);
+
 /* The same pass as fira_step() (Algorithm 1's loop body) for callers whose weights
  * and gradients live in HOST memory: W_host and G_host are host arrays of `count`
  * host pointers (m x ld elements each; page-locked memory makes the copies

@@ -108,6 +108,12 @@ SIGNATURES = {
     "fira_embedding_grad": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_int64, C.c_int64,
                                       C.c_float, C.c_void_p, C.c_int64, C.c_int, C.c_int32, C.c_void_p, C.c_size_t,
                                       C.c_void_p]),
+    "fira_layer_norm": (C.c_int, [C.c_void_p, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_int,
+                                  C.c_float, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "fira_layer_norm_grad_work_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int]),
+    "fira_layer_norm_grad": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_void_p,
+                                       C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                       C.c_int, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
     "fira_status_string": (C.c_char_p, [C.c_int]),
     "fira_last_error": (C.c_char_p, []),
     "fira_destroy": (None, [C.c_void_p]),
@@ -313,6 +319,11 @@ def _pitch(t: torch.Tensor, what: str) -> int:
     raise ValueError(f"{what}: strides {tuple(t.stride())} of shape {tuple(t.shape)}: rows of one pitch are needed")
 
 
+def _address(t: torch.Tensor):
+    """A tensor's address; of an empty one, which has none, one that is not NULL and that nothing is read from."""
+    return t.data_ptr() or 256
+
+
 def _same_device(device: torch.device, **tensors: Optional[torch.Tensor]) -> None:
     for name, t in tensors.items():
         if t is not None and t.device != device:
@@ -369,6 +380,89 @@ def embedding_grad(tokens: torch.Tensor, dY: torch.Tensor, vocab: int, scale: fl
                                         1 if accumulate else 0, work.data_ptr(), work.numel() * work.element_size(),
                                         torch.cuda.current_stream().cuda_stream))
     return out
+
+
+def _check_params(hidden: int, gain: torch.Tensor, bias: Optional[torch.Tensor], what: str) -> int:
+    code = _code(gain, what)
+    for p in (gain, bias):
+        if p is not None and (p.shape != (hidden,) or not p.is_contiguous() or p.dtype != gain.dtype):
+            raise ValueError(f"{what}: contiguous vectors of {hidden} elements of one type are needed, not {tuple(p.shape)} "
+                             f"of {p.dtype}")
+    return code
+
+
+def _check_stats(rows: int, mean: Optional[torch.Tensor], rstd: torch.Tensor, rms: bool) -> None:
+    if (mean is None) != rms:
+        raise ValueError("mean is None in the form without mean, and needed in the other")
+    for t in (mean, rstd):
+        if t is not None and (t.numel() != rows or t.dtype != torch.float32 or not t.is_contiguous()):
+            raise ValueError(f"mean and rstd: {rows} contiguous float32 numbers are needed")
+
+
+def layer_norm(x: torch.Tensor, gain: torch.Tensor, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+               rms: bool = False, out: Optional[torch.Tensor] = None):
+    """fira_layer_norm over the last dimension: (y, mean, rstd); rms: the form without mean and bias (mean is None).  mean
+    and rstd are float32 of x's other dimensions, for layer_norm_grad.  out: may be x itself."""
+    code = _code(x, "x")
+    if x.dim() == 0 or x.shape[-1] == 0:
+        raise ValueError(f"x has no rows: {tuple(x.shape)}")
+    device, hidden = x.device, x.shape[-1]
+    params = _check_params(hidden, gain, bias, "gain and bias")
+    _same_device(device, gain=gain, bias=bias, out=out)
+    ld = _pitch(x, "x")
+    with _on(device):
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=device)
+        elif out.shape != x.shape or out.dtype != x.dtype:
+            raise ValueError(f"out: {tuple(x.shape)} of {x.dtype} is needed, not {tuple(out.shape)} of {out.dtype}")
+        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=device)
+        mean = None if rms else torch.empty_like(rstd)
+        check(lib().fira_layer_norm(x.data_ptr(), ld, code, rstd.numel(), hidden, gain.data_ptr(),
+                                    None if bias is None else bias.data_ptr(), params, eps, out.data_ptr(), _pitch(out, "out"),
+                                    None if rms else _address(mean), _address(rstd), torch.cuda.current_stream().cuda_stream))
+    return out, mean, rstd
+
+
+def layer_norm_grad(dY: torch.Tensor, x: torch.Tensor, gain: torch.Tensor, mean: Optional[torch.Tensor], rstd: torch.Tensor,
+                    rms: bool = False, out: Optional[torch.Tensor] = None, dgain: Optional[torch.Tensor] = None,
+                    dbias: Optional[torch.Tensor] = None, accumulate: bool = False, work: Optional[torch.Tensor] = None):
+    """fira_layer_norm_grad: (dX, dgain, dbias) from the gradient of y and from what layer_norm returned; dbias is None in
+    the form without mean.  out (dX): may be dY or x itself.  dgain, dbias: float32 or bfloat16, by default new tensors of the gain's type;
+    accumulate: added to what is in them.  work: a byte tensor of at least lib().fira_layer_norm_grad_work_bytes() bytes; by
+    default torch's allocator lends one for the call."""
+    code = _code(x, "x")
+    if x.dim() == 0 or x.shape[-1] == 0 or dY.shape != x.shape or dY.dtype != x.dtype:
+        raise ValueError(f"dY {tuple(dY.shape)} of {dY.dtype} for x {tuple(x.shape)} of {x.dtype}")
+    device, hidden = x.device, x.shape[-1]
+    rows = x.numel() // hidden
+    params = _check_params(hidden, gain, None, "gain")
+    _check_stats(rows, mean, rstd, rms)
+    if rms and dbias is not None:
+        raise ValueError("the form without mean has no bias")
+    if accumulate and (dgain is None or (dbias is None and not rms)):
+        raise ValueError("accumulate: dgain and dbias are needed")
+    _same_device(device, dY=dY, gain=gain, mean=mean, rstd=rstd, out=out, dgain=dgain, dbias=dbias, work=work)
+    ld = _pitch(x, "x")
+    with _on(device):
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=device)
+        elif out.shape != x.shape or out.dtype != x.dtype:
+            raise ValueError(f"out: {tuple(x.shape)} of {x.dtype} is needed, not {tuple(out.shape)} of {out.dtype}")
+        if not (dY.is_contiguous() or (dY.dim() == 2 and dY.stride(1) == 1 and dY.stride(0) >= hidden)):
+            dY = dY.contiguous()
+        if dgain is None:
+            dgain = torch.empty_like(gain)
+        if dbias is None and not rms:
+            dbias = torch.empty_like(dgain)
+        grads = _check_params(hidden, dgain, dbias, "dgain and dbias")
+        if work is None:
+            work = torch.empty(lib().fira_layer_norm_grad_work_bytes(rows, hidden, code) or 1, dtype=torch.uint8, device=device)
+        check(lib().fira_layer_norm_grad(dY.data_ptr(), _pitch(dY, "dY"), x.data_ptr(), ld, code, rows, hidden, gain.data_ptr(),
+                                         params, None if rms else _address(mean), rstd.data_ptr(), out.data_ptr(),
+                                         _pitch(out, "out"), dgain.data_ptr(), None if rms else dbias.data_ptr(), grads,
+                                         1 if accumulate else 0, work.data_ptr(), work.numel() * work.element_size(),
+                                         torch.cuda.current_stream().cuda_stream))
+    return out, dgain, dbias
 
 
 class Fira:
