@@ -26,7 +26,8 @@ constexpr int GC_UNROLL = 4;                      // chunks of a thread in fligh
 constexpr int GC_TILE = GC_THREADS * GC_UNROLL;   // chunks of a tile (8192 elements)
 constexpr int GC_SMS = 148;
 constexpr int GC_BLOCKS = GC_SMS * 4;             // blocks of a launch: tiles are dealt to them in turn
-constexpr int GC_MANY = 512, GC_FEW = 48;         // tensors of a launch: 28 KB of kernel arguments, or 2.7 KB
+constexpr int GC_MANY = 480, GC_FEW = 48;         // tensors of a launch: 31 KB of kernel arguments, or 3.1 KB
+constexpr long long GC_KEPT = 80ll << 20;         // bytes that the scaling finds in L2 (126 MB, which its stores share)
 
 // One tensor.  A flat one is one row; rows of a pitched one start on their own.
 struct GradEntry {
@@ -39,6 +40,7 @@ struct GradEntry {
   unsigned char bf16, out_bf16;
   unsigned char single;     // a chunk is one element: rows that do not start on 16-byte boundaries
   unsigned char pitched;
+  long long whole;          // tiles from the first on that are GC_TILE whole chunks in a row (the others go chunk by chunk)
 };
 
 template <int CAP>
@@ -122,6 +124,30 @@ __device__ __forceinline__ void store_chunk(const GradEntry& t, const Place& p, 
   }
 }
 
+// L2 policies.  What is read once or written for somebody later makes room for what the scaling reads again.
+__device__ __forceinline__ uint64_t policy(bool first) {
+  uint64_t p;
+  if (first) asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  else asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ uint4 load16(const void* p, uint64_t pol) {
+  uint4 u;
+  asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.b32 {%0, %1, %2, %3}, [%4], %5;"
+               : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p), "l"(pol));
+  return u;
+}
+__device__ __forceinline__ void store16(void* p, const uint4& u, uint64_t pol) {
+  asm volatile("st.global.L2::cache_hint.v4.b32 [%0], {%1, %2, %3, %4}, %5;" :: "l"(p), "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w), "l"(pol) : "memory");
+}
+__device__ __forceinline__ void store8(void* p, unsigned x, unsigned y, uint64_t pol) {
+  asm volatile("st.global.L2::cache_hint.v2.b32 [%0], {%1, %2}, %3;" :: "l"(p), "r"(x), "r"(y), "l"(pol) : "memory");
+}
+__device__ __forceinline__ unsigned pack2(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const unsigned*>(&h);
+}
+
 // The chunks of this thread in a tile.
 struct Tile {
   int q;                       // tensor
@@ -157,6 +183,75 @@ __device__ __forceinline__ void load_tile(const GradEntry* tab, const Tile& x, P
   }
 }
 
+// Whole tiles: 16 bytes per thread and load, W of them (4: bf16, 8: fp32).
+template <int W>
+__device__ __forceinline__ void load_whole(const void* g, long long first, uint64_t pol, uint4 (&u)[W]) {
+  const uint4* p = static_cast<const uint4*>(g) + first * (W / GC_UNROLL) + threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < W; ++i) u[i] = load16(p + i * GC_THREADS, pol);
+}
+template <int W>
+__device__ __forceinline__ void unpack_whole(const uint4& u, float* v) {
+  const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (W == 8) v[k] = __uint_as_float(w[k]);
+    else { v[2 * k] = __uint_as_float(w[k] << 16); v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u); }
+  }
+}
+constexpr int GC_ELEMS = GC_UNROLL * GC_CHUNK;     // of a thread in a tile
+
+// The sum of the squares of a thread's elements of a tile.
+__device__ __forceinline__ double squares(const float (&v)[GC_ELEMS]) {
+  float s = 0.f;
+#pragma unroll
+  for (int e = 0; e < GC_ELEMS; ++e) s = fmaf(v[e], v[e], s);
+  if (s >= 0x1p-80f && s <= 0x1p126f) return (double)s;      // what underflowed is below 32 * 2^-126, the rounding below 32 * 2^-24 of s
+  bool any = false;
+#pragma unroll
+  for (int e = 0; e < GC_ELEMS; ++e) any |= v[e] != 0.f;
+  double d = 0.0;
+  if (any) {
+#pragma unroll
+    for (int e = 0; e < GC_ELEMS; ++e) d = fma((double)v[e], (double)v[e], d);
+  }
+  return d;
+}
+template <int W>
+__device__ __forceinline__ double whole_squares(const void* g, long long first, uint64_t pol) {
+  uint4 u[W];
+  load_whole<W>(g, first, pol, u);
+  float v[GC_ELEMS];
+#pragma unroll
+  for (int i = 0; i < W; ++i) unpack_whole<W>(u[i], v + i * (GC_ELEMS / W));
+  return squares(v);
+}
+template <int W, bool OUT_BF16>
+__device__ __forceinline__ void whole_scale(const void* g, void* o, long long first, float scale, uint64_t load_pol, uint64_t store_pol) {
+  uint4 u[W];
+  load_whole<W>(g, first, load_pol, u);
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    constexpr int N = GC_ELEMS / W;
+    float v[N];
+    unpack_whole<W>(u[i], v);
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] *= scale;
+    // the 16 bytes that were read, seen as elements of the tensor
+    const long long at = (first * (W / GC_UNROLL) + i * GC_THREADS + threadIdx.x) * N;
+    if constexpr (OUT_BF16) {
+      __nv_bfloat16* q = static_cast<__nv_bfloat16*>(o) + at;
+      if constexpr (N == 8) store16(q, make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])), store_pol);
+      else store8(q, pack2(v[0], v[1]), pack2(v[2], v[3]), store_pol);
+    } else {
+      float* q = static_cast<float*>(o) + at;
+#pragma unroll
+      for (int e = 0; e < N; e += 4)
+        store16(q + e, make_uint4(__float_as_uint(v[e]), __float_as_uint(v[e + 1]), __float_as_uint(v[e + 2]), __float_as_uint(v[e + 3])), store_pol);
+    }
+  }
+}
+
 __device__ __forceinline__ double block_sum(double s, double* smem) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -170,37 +265,24 @@ __device__ __forceinline__ double block_sum(double s, double* smem) {
 
 template <int CAP>
 __global__ void __launch_bounds__(GC_THREADS, 4)
-k_grad_squares(const __grid_constant__ GradTable<CAP> tab, double* __restrict__ sums) {
+k_grad_squares(const __grid_constant__ GradTable<CAP> tab, double* __restrict__ sums, int kept) {
   __shared__ double red[GC_THREADS / 32];
   ptx::grid_launch_next();     // its blocks take the places that ours leave, and wait for the last of ours
+  const uint64_t once = policy(true), again = policy(false);
   double total = 0.0;
   int q = 0;
   for (int tile = blockIdx.x; tile < tab.tiles; tile += gridDim.x) {
     while (q + 1 < tab.count && tile >= tab.t[q + 1].tile_start) ++q;
-    Place p[GC_UNROLL];
-    float v[GC_UNROLL][8];
-    load_tile(tab.t, open_tile(tab.t, q, tile), p, v);
-    float s = 0.f;
-#pragma unroll
-    for (int u = 0; u < GC_UNROLL; ++u)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s = fmaf(v[u][e], v[u][e], s);
-    if (s >= 0x1p-80f && s <= 0x1p126f) {
-      total += (double)s;      // what underflowed is below 32 * 2^-126, the rounding below 32 * 2^-24 of s
+    const GradEntry& t = tab.t[q];
+    if (tile - t.tile_start < t.whole) {
+      const uint64_t pol = tile >= kept ? again : once;
+      const long long first = (long long)(tile - t.tile_start) * GC_TILE;
+      total += t.bf16 ? whole_squares<4>(t.g, first, pol) : whole_squares<8>(t.g, first, pol);
     } else {
-      bool any = false;
-#pragma unroll
-      for (int u = 0; u < GC_UNROLL; ++u)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) any |= v[u][e] != 0.f;
-      if (any) {
-        double d = 0.0;
-#pragma unroll
-        for (int u = 0; u < GC_UNROLL; ++u)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) d = fma((double)v[u][e], (double)v[u][e], d);
-        total += d;
-      }
+      Place p[GC_UNROLL];
+      float v[GC_UNROLL][8];
+      load_tile(tab.t, open_tile(tab.t, q, tile), p, v);
+      total += squares(reinterpret_cast<const float (&)[GC_ELEMS]>(v));
     }
   }
   const double r = block_sum(total, red);
@@ -224,8 +306,8 @@ k_grad_norm(const double* sums, int nsums, float* norm_out) {
 
 template <int CAP>
 __global__ void __launch_bounds__(GC_THREADS, 4)
-k_grad_scale(const __grid_constant__ GradTable<CAP> tab, const double* sums, int nsums, float max_norm,
-             float* norm_out, float* scale_out, int in_place) {
+k_grad_scale(const __grid_constant__ GradTable<CAP> tab, const double* sums, int nsums, float max_norm, float* norm_out, float* scale_out,
+             int in_place, int kept) {
   __shared__ double red[GC_THREADS / 32];
   ptx::grid_wait();
   const double norm = norm_of(sums, nsums, red);
@@ -233,18 +315,32 @@ k_grad_scale(const __grid_constant__ GradTable<CAP> tab, const double* sums, int
   const float scale = finite && norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.f;
   if (blockIdx.x == 0 && threadIdx.x == 0) { *norm_out = (float)norm; *scale_out = scale; }
   if (in_place && scale == 1.f) return;
+  const uint64_t once = policy(true), later = policy(false);
   int q = tab.count - 1;
   // from the end: what the sums read last is what the L2 still holds
   for (int tile = tab.tiles - 1 - (int)blockIdx.x; tile >= 0; tile -= gridDim.x) {
     while (tile < tab.t[q].tile_start) --q;
-    Place p[GC_UNROLL];
-    float v[GC_UNROLL][8];
-    load_tile(tab.t, open_tile(tab.t, q, tile), p, v);
+    const GradEntry& t = tab.t[q];
+    if (tile - t.tile_start < t.whole) {
+      const long long first = (long long)(tile - t.tile_start) * GC_TILE;
+      const uint64_t pol = tile >= kept ? once : later;       // (no store takes the place of what is still to be read)
+      if (t.bf16) {
+        if (t.out_bf16) whole_scale<4, true>(t.g, t.o, first, scale, once, pol);
+        else whole_scale<4, false>(t.g, t.o, first, scale, once, pol);
+      } else {
+        if (t.out_bf16) whole_scale<8, true>(t.g, t.o, first, scale, once, pol);
+        else whole_scale<8, false>(t.g, t.o, first, scale, once, pol);
+      }
+    } else {
+      Place p[GC_UNROLL];
+      float v[GC_UNROLL][8];
+      load_tile(tab.t, open_tile(tab.t, q, tile), p, v);
 #pragma unroll
-    for (int u = 0; u < GC_UNROLL; ++u) {
+      for (int u = 0; u < GC_UNROLL; ++u) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[u][e] *= scale;
-      if (p[u].len) store_chunk(tab.t[q], p[u], v[u]);
+        for (int e = 0; e < 8; ++e) v[u][e] *= scale;
+        if (p[u].len) store_chunk(t, p[u], v[u]);
+      }
     }
   }
 }
@@ -324,10 +420,24 @@ void fill(GradTable<CAP>& tab, int base, int n, const fira_grad_desc* descs, con
     t.single = (((uintptr_t)t.g | (uintptr_t)t.o) & 15) != 0 || (t.pitched && ((ld * es | out_ld * os) & 15) != 0);
     const long long w = t.single ? 1 : GC_CHUNK;
     t.chunks = (t.pitched ? d.rows : 1) * ((t.n + w - 1) / w);
+    t.whole = t.pitched || t.single ? 0 : t.n / GC_CHUNK / GC_TILE;
     t.tile_start = (int)tiles;
     tiles += (t.chunks + GC_TILE - 1) / GC_TILE;
   }
   tab.tiles = (int)tiles;
+}
+
+// The first tile from which on the list's bytes fit what the L2 is expected to keep.
+template <int CAP>
+int kept_from(const GradTable<CAP>& tab) {
+  long long bytes = 0;
+  for (int q = tab.count - 1; q >= 0; --q) {
+    const long long per_tile = (long long)GC_TILE * (tab.t[q].single ? 1 : GC_CHUNK) * (tab.t[q].bf16 ? 2 : 4);
+    const long long tiles = (q + 1 < tab.count ? tab.t[q + 1].tile_start : tab.tiles) - tab.t[q].tile_start;
+    if (bytes + tiles * per_tile > GC_KEPT) return tab.t[q].tile_start + (int)(tiles - (GC_KEPT - bytes) / per_tile);
+    bytes += tiles * per_tile;
+  }
+  return 0;
 }
 
 // out_dev null: in place.  scale_dev null: the norm alone.
@@ -339,7 +449,7 @@ cudaError_t run_list(int32_t count, const fira_grad_desc* descs, const void* con
   for (int base = 0; base < count; base += CAP) {
     fill(tab, base, std::min(CAP, count - base), descs, G_dev, out_dev);
     const int blocks = std::max(1, std::min(GC_BLOCKS, tab.tiles));
-    k_grad_squares<CAP><<<blocks, GC_THREADS, 0, st>>>(tab, sums + nsums);
+    k_grad_squares<CAP><<<blocks, GC_THREADS, 0, st>>>(tab, sums + nsums, scale_dev ? kept_from(tab) : tab.tiles);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     nsums += blocks;
@@ -350,7 +460,7 @@ cudaError_t run_list(int32_t count, const fira_grad_desc* descs, const void* con
     if (count > CAP) fill(tab, base, std::min(CAP, count - base), descs, G_dev, out_dev);
     const int blocks = std::max(1, std::min(GC_BLOCKS, tab.tiles));
     const cudaError_t e = launch_chained(k_grad_scale<CAP>, dim3(blocks), GC_THREADS, 0, st, chained, 1, tab, (const double*)sums, nsums,
-                                         max_norm, norm_dev, scale_dev, out_dev == nullptr ? 1 : 0);
+                                         max_norm, norm_dev, scale_dev, out_dev == nullptr ? 1 : 0, kept_from(tab));
     if (e != cudaSuccess) return e;
     chained = false;
   }
