@@ -3,12 +3,13 @@
 //   Y_i = a E[t_i]                         (t_i outside 0 .. vocab-1: a row of zeros)
 //   dE_v = a sum over {i : t_i = v} of dY_i
 //
-// The gradient takes two launches.  k_token_order sorts the positions by token: each block owns a range of tokens and
-// reads all tokens of the batch (they stay in L2: 148 blocks x 512 KB at 131072 tokens), counts those below its range,
-// which is where its own positions begin in the sorted order, and those of each row of its range, and then stores
-// its positions.  No block waits for another, and the order is the same in every call.
-// k_table_grad sums: a warp takes T sorted positions and a slice of columns, whole rows of the table where a row has
-// at most T positions (the warp in whose range it begins does all of it).  A row with more, as words at the top of a
+// The gradient takes two launches.  k_token_order groups the positions by token: each block owns the tokens of one
+// remainder by the number of blocks (so that the frequent ones, which in most vocabularies lie side by side, fall to different blocks)
+// and reads all tokens of the batch, which stay in L2.  It counts those of lower remainders, which is where its own
+// positions begin, and lists its own in shared memory; then it sorts the list by row.  No block waits for another, and the
+// order is the same in every call.
+// k_table_grad sums: a warp takes T positions of that order and a slice of columns, whole rows of the table where a row has
+// at most T positions (the warp in whose stretch it begins does all of it).  A row with more, as words at the top of a
 // Zipf law have, is cut at the multiples of T; the parts are stored, and the warp that comes last, by a counter, adds them
 // in their order.  Rows without a token are zeroed by warps of the same launch.  Sums are fp32, rounded once.
 #include <math.h>
@@ -79,29 +80,34 @@ k_embedding(const T* __restrict__ table, long long ld, const TOK* __restrict__ t
 }
 
 // ------------------------------------------------------------------------------------------------ order of the tokens
-constexpr int ORD_THREADS = 1024;
-constexpr int ORD_WARPS = ORD_THREADS / 32;
-constexpr int ORD_MAX_ROWS = 1024;          // rows of a block's range: a thread each, and 128 KB of counts
+constexpr int ORD_MIN_BLOCKS = 128;         // a power of two: a remainder is a few low bits
+constexpr int ORD_MAX_ROWS = 1024;          // rows of a block
+constexpr int ORD_MAX_THREADS = 1024;
 constexpr int ORD_STEP = 128;               // tokens of a warp's step: four per lane
+constexpr int ORD_LIST = 256;               // entries of a warp's list
 
-// Four tokens from position i on (-1 behind the end and where a token is none of the table's).
+// Four tokens from position i on: 0xffffffff behind the end and where a token is none of the table's.
 template <typename TOK, bool VECTOR>
-__device__ __forceinline__ void load_tokens(const TOK* __restrict__ tokens, int i, int n, int vocab, int (&t)[4]) {
-  long long x[4] = {-1, -1, -1, -1};
+__device__ __forceinline__ void load_tokens(const TOK* __restrict__ tokens, int i, int n, int vocab, unsigned (&t)[4]) {
+  unsigned high[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) t[j] = 0xffffffffu;
   if (VECTOR && i + 4 <= n) {
+    const uint4 u = reinterpret_cast<const uint4*>(tokens + i)[0];
     if constexpr (sizeof(TOK) == 4) {
-      const int4 u = *reinterpret_cast<const int4*>(tokens + i);
-      x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
+      t[0] = u.x; t[1] = u.y; t[2] = u.z; t[3] = u.w;
     } else {
-      const longlong2 a = reinterpret_cast<const longlong2*>(tokens + i)[0], b = reinterpret_cast<const longlong2*>(tokens + i)[1];
-      x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
+      const uint4 w = reinterpret_cast<const uint4*>(tokens + i)[1];
+      t[0] = u.x; t[1] = u.z; t[2] = w.x; t[3] = w.z;
+      high[0] = u.y; high[1] = u.w; high[2] = w.y; high[3] = w.w;
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) if (i + j < n) x[j] = (long long)tokens[i + j];
+    for (int j = 0; j < 4; ++j)
+      if (i + j < n) { t[j] = (unsigned)tokens[i + j]; if (sizeof(TOK) == 8) high[j] = (unsigned)((unsigned long long)tokens[i + j] >> 32); }
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) t[j] = x[j] >= 0 && x[j] < vocab ? (int)x[j] : -1;
+  for (int j = 0; j < 4; ++j) t[j] = t[j] < (unsigned)vocab && high[j] == 0u ? t[j] : 0xffffffffu;
 }
 
 __device__ __forceinline__ unsigned warp_inclusive(unsigned x) {
@@ -113,150 +119,194 @@ __device__ __forceinline__ unsigned warp_inclusive(unsigned x) {
   return x;
 }
 
-// order: (position, token) sorted by token; start[v]: where row v begins, start[vocab]: tokens of the table in the batch.
+// Stores the positions of up to 32 entries (a lane's own: row r where `in`) at the places that `mine` counts.
+__device__ __forceinline__ void place_entries(bool in, unsigned r, int position, int token, unsigned* mine, int2* order) {
+  const int lane = threadIdx.x & 31;
+  const unsigned same = __match_any_sync(0xffffffffu, in ? r : 0x80000000u | lane);
+  const unsigned at = in ? mine[r] : 0u;
+  __syncwarp();
+  if (in) {
+    order[at + __popc(same & ((1u << lane) - 1))] = make_int2(position, token);
+    if (lane == __ffs(same) - 1) mine[r] = at + __popc(same);
+  }
+  __syncwarp();
+}
+
+// order: (position, token), equal tokens together; span[v]: where those of v begin and end; *total: tokens of the table.
 // Among equal tokens the order goes by warp (a stretch of positions each), step, place in the lane's four, lane.
+// Block b has the tokens v with v & (gridDim - 1) = b, in rows v >> shift.
 template <typename TOK, bool VECTOR>
-__global__ void __launch_bounds__(ORD_THREADS)
-k_token_order(const TOK* __restrict__ tokens, int n, int vocab, int range, int2* __restrict__ order, int* __restrict__ start,
-              unsigned* __restrict__ counters, long long ncounters) {
-  extern __shared__ unsigned cnt[];         // [ORD_WARPS][range]
-  __shared__ unsigned below_s[ORD_WARPS], sum_s[ORD_WARPS];
+__global__ void __launch_bounds__(ORD_MAX_THREADS)
+k_token_order(const TOK* __restrict__ tokens, int n, int vocab, int shift, int nrows, int2* __restrict__ order, int2* __restrict__ span,
+              int* __restrict__ total, unsigned* __restrict__ counters, long long ncounters) {
+  extern __shared__ unsigned shared[];      // counts [warps][nrows], lists [warps][ORD_LIST] of (position, row)
+  __shared__ unsigned below_s[32], sum_s[32];
   ptx::grid_launch_next();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int v0 = blockIdx.x * range;        // (grid: ceil(vocab / range) blocks, so v0 < vocab)
-  const unsigned here = (unsigned)min(range, vocab - v0);
-  for (long long i = (long long)blockIdx.x * ORD_THREADS + threadIdx.x; i < ncounters; i += (long long)gridDim.x * ORD_THREADS) counters[i] = 0;
-  for (int i = threadIdx.x; i < ORD_WARPS * range; i += ORD_THREADS) cnt[i] = 0;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, threads = blockDim.x;
+  const unsigned me = blockIdx.x, mask = gridDim.x - 1;
+  for (long long i = (long long)blockIdx.x * threads + threadIdx.x; i < ncounters; i += (long long)gridDim.x * threads) counters[i] = 0;
+  unsigned* mine = shared + warp * nrows;
+  int2* list = reinterpret_cast<int2*>(shared + ((warps * nrows + 1) & ~1)) + warp * ORD_LIST;
+  for (int i = threadIdx.x; i < warps * nrows; i += threads) shared[i] = 0;
   __syncthreads();
-  unsigned* mine = cnt + warp * range;
-  const int steps = (n + ORD_STEP - 1) / ORD_STEP, per_warp = (steps + ORD_WARPS - 1) / ORD_WARPS;
+  const int steps = (n + ORD_STEP - 1) / ORD_STEP, per_warp = (steps + warps - 1) / warps;
   const int s0 = min(steps, warp * per_warp), s1 = min(steps, s0 + per_warp);
   unsigned below = 0;
-#pragma unroll 4
+  int listed = 0;                           // entries of this warp, whether the list holds them or not
+  unsigned next[4];
+  load_tokens<TOK, VECTOR>(tokens, s0 * ORD_STEP + lane * 4, s0 < s1 ? n : 0, vocab, next);
   for (int s = s0; s < s1; ++s) {
-    int t[4];
-    load_tokens<TOK, VECTOR>(tokens, s * ORD_STEP + lane * 4, n, vocab, t);
+    unsigned t[4], home[4];                 // home of a position without a token: no block's
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      below += (unsigned)t[j] < (unsigned)v0;
-      const unsigned r = (unsigned)t[j] - (unsigned)v0;
-      if (r < here) atomicAdd(&mine[r], 1u);
+      t[j] = next[j];
+      home[j] = t[j] == 0xffffffffu ? t[j] : t[j] & mask;
+      below += home[j] < me;
+    }
+    if (s + 1 < s1) load_tokens<TOK, VECTOR>(tokens, (s + 1) * ORD_STEP + lane * 4, n, vocab, next);
+    if (!__any_sync(0xffffffffu, home[0] == me || home[1] == me || home[2] == me || home[3] == me)) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const unsigned found = __ballot_sync(0xffffffffu, home[j] == me);
+      if (home[j] == me) {
+        const unsigned r = t[j] >> shift;
+        atomicAdd(&mine[r], 1u);
+        const int k = listed + __popc(found & ((1u << lane) - 1));
+        if (k < ORD_LIST) list[k] = make_int2(s * ORD_STEP + lane * 4 + j, (int)r);
+      }
+      listed += __popc(found);
     }
   }
   below = __reduce_add_sync(0xffffffffu, below);
   if (lane == 0) below_s[warp] = below;
   __syncthreads();
-  below = __reduce_add_sync(0xffffffffu, below_s[lane]);
-  const unsigned r = threadIdx.x;
-  unsigned total = 0;
-  if (r < here)
-    for (int w = 0; w < ORD_WARPS; ++w) {
-      const unsigned c = cnt[w * range + r];
-      cnt[w * range + r] = total;
-      total += c;
+  unsigned front = 0;                       // positions in front of the rows that are summed next
+  for (int w = 0; w < warps; ++w) front += below_s[w];
+  for (int base = 0; base < nrows; base += threads) {
+    const int r = base + threadIdx.x;
+    unsigned count = 0;
+    if (r < nrows) {
+#pragma unroll 8
+      for (int w = 0; w < warps; ++w) {
+        const unsigned c = shared[w * nrows + r];
+        shared[w * nrows + r] = count;
+        count += c;
+      }
     }
-  const unsigned inclusive = warp_inclusive(total);
-  if (lane == 31) sum_s[warp] = inclusive;
-  __syncthreads();
-  const unsigned sums = warp_inclusive(sum_s[lane]);
-  const unsigned in_front = __shfl_sync(0xffffffffu, sums, max(warp - 1, 0));
-  const unsigned front = below + (warp ? in_front : 0u) + inclusive - total;
-  if (r < here) {
-    start[v0 + r] = (int)front;
-    if (v0 + (int)r == vocab - 1) start[vocab] = (int)(front + total);
-    for (int w = 0; w < ORD_WARPS; ++w) cnt[w * range + r] += front;
+    const unsigned inclusive = warp_inclusive(count);
+    if (lane == 31) sum_s[warp] = inclusive;
+    __syncthreads();
+    unsigned at = front + inclusive - count;
+    for (int w = 0; w < warps; ++w) {
+      if (w < warp) at += sum_s[w];
+      front += sum_s[w];
+    }
+    if (r < nrows) {
+      const long long v = ((long long)r << shift) + me;
+      if (v < vocab) span[v] = make_int2((int)at, (int)(at + count));
+#pragma unroll 8
+      for (int w = 0; w < warps; ++w) shared[w * nrows + r] += at;
+    }
+    __syncthreads();
   }
-  __syncthreads();
-#pragma unroll 2
-  for (int s = s0; s < s1; ++s) {
-    int t[4];
-    const int i = s * ORD_STEP + lane * 4;
-    load_tokens<TOK, VECTOR>(tokens, i, n, vocab, t);
+  if (me == mask && threadIdx.x == 0) *total = (int)front;
+  if (listed <= ORD_LIST) {
+    for (int k = 0; k < listed; k += 32) {
+      const bool in = k + lane < listed;
+      const int2 e = in ? list[k + lane] : make_int2(0, 0);
+      place_entries(in, (unsigned)e.y, e.x, (int)(((unsigned)e.y << shift) + me), mine, order);
+    }
+  } else {
+    for (int s = s0; s < s1; ++s) {
+      unsigned t[4];
+      const int i = s * ORD_STEP + lane * 4;
+      load_tokens<TOK, VECTOR>(tokens, i, n, vocab, t);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const unsigned k = (unsigned)t[j] - (unsigned)v0;
-      const bool in = k < here;
-      if (__any_sync(0xffffffffu, in)) {
-        const unsigned same = __match_any_sync(0xffffffffu, in ? k : 0x80000000u | lane);
-        const unsigned at = in ? mine[k] : 0u;
-        __syncwarp();
-        if (in) {
-          order[at + __popc(same & ((1u << lane) - 1))] = make_int2(i + j, t[j]);
-          if (lane == __ffs(same) - 1) mine[k] = at + __popc(same);
-        }
-        __syncwarp();
+      for (int j = 0; j < 4; ++j) {
+        const bool in = t[j] != 0xffffffffu && (t[j] & mask) == me;
+        if (__any_sync(0xffffffffu, in)) place_entries(in, t[j] >> shift, i + j, (int)t[j], mine, order);
       }
     }
   }
 }
 
 // ------------------------------------------------------------------------------------------------ sums of the rows
-constexpr int TG_UNROLL = 8;                // rows of dY in flight
-constexpr int TG_ZERO_ROWS = 16;            // rows that a warp looks over for tokens
+constexpr int TG_DEPTH = 4;                 // rows of dY of a warp on their way
+constexpr int TG_MIN = 16;                  // positions of a stretch at least
+constexpr int TG_ZERO_ROWS = 64;            // rows that a block looks over for tokens
+constexpr int TG_ZERO_EARLY = 16384;        // tokens up to which such a block looks through them itself
 
 struct TablePlan {
-  int range, blocks;                        // k_token_order
-  int T;                                    // sorted positions of a warp
-  long long chunks;
-  int slices;
-  size_t off_start, off_counters, off_parts, bytes;
+  int shift, blocks, nrows, threads;        // k_token_order
+  long long chunks;                         // stretches of the order
+  int slices, pieces;
+  size_t off_span, off_total, off_counters, off_parts, bytes;
 };
 
-template <typename TI, typename TO, bool VECTOR>
+// The columns of a warp: PIECES times 32 lanes of 16 bytes of dY.
+template <typename TI, typename TO, bool VECTOR, int PIECES>
 struct Slice {
-  static constexpr int N = rows::PER16<TI>;
+  static constexpr int E = rows::PER16<TI>, N = E * PIECES, WIDTH = 32 * N;
   int col0, lane, hidden;
-  struct alignas(16) Piece { TI v[N]; };                // as it was read: 16 bytes, converted where it is added
-  __device__ __forceinline__ void load(const TI* row, Piece& p) const {
-    if (VECTOR) {
-      if (col0 + lane * N < hidden) *reinterpret_cast<uint4*>(&p) = *reinterpret_cast<const uint4*>(row + col0 + lane * N);
-    } else {
+  __device__ __forceinline__ int col(int p, int e) const { return col0 + p * 32 * E + (VECTOR ? lane * E + e : e * 32 + lane); }
+  // A row on its way to a slot, of which a lane reads its own.
+  __device__ __forceinline__ void fetch(const TI* row, uint4* slot) const {
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const int c = col0 + e * 32 + lane;
-        if (c < hidden) p.v[e] = row[c];
+    for (int p = 0; p < PIECES; ++p) {
+      if (VECTOR) {
+        if (col(p, 0) < hidden)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"((unsigned)__cvta_generic_to_shared(slot + p * 32 + lane)), "l"(row + col(p, 0)) : "memory");
+      } else {
+        TI* v = reinterpret_cast<TI*>(slot + p * 32 + lane);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (col(p, e) < hidden) v[e] = row[col(p, e)];
       }
     }
   }
-  __device__ __forceinline__ void add(const Piece& p, float (&sum)[N]) const {
-    float v[N];
-    rows::unpack<TI>(*reinterpret_cast<const uint4*>(&p), v);
+  __device__ __forceinline__ void add(const uint4* slot, float (&sum)[N]) const {
 #pragma unroll
-    for (int e = 0; e < N; ++e) sum[e] += v[e];
+    for (int p = 0; p < PIECES; ++p) {
+      float v[E];
+      rows::unpack<TI>(slot[p * 32 + lane], v);         // (columns beyond the width: whatever is there, never stored)
+#pragma unroll
+      for (int e = 0; e < E; e += 2) rows::add2(sum[p * E + e], sum[p * E + e + 1], v[e], v[e + 1]);
+    }
   }
-  __device__ __forceinline__ void store(TO* row, float (&v)[N], float scale, bool add) const {
-    if (VECTOR) {
-      if (col0 + lane * N >= hidden) return;
-      TO* p = row + col0 + lane * N;
-      if constexpr (N * sizeof(TO) % 16 == 0) {
-        float old[N];
-        if (add) rows::load_vec<TO, N>(p, old);
+  __device__ __forceinline__ void store(TO* row, float (&sum)[N], float scale, bool add) const {
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = add ? fmaf(scale, v[e], old[e]) : scale * v[e];
-        rows::store_vec<TO, N>(p, v);
-      } else {                              // fp32 rows into bf16: 8 bytes
-        static_assert(N == 4 && sizeof(TO) == 2, "");
-        uint2* q = reinterpret_cast<uint2*>(p);
-        float old[4] = {0.f, 0.f, 0.f, 0.f};
-        if (add) {
-          const uint2 u = *q;
-          old[0] = __uint_as_float(u.x << 16); old[1] = __uint_as_float(u.x & 0xffff0000u);
-          old[2] = __uint_as_float(u.y << 16); old[3] = __uint_as_float(u.y & 0xffff0000u);
+    for (int p = 0; p < PIECES; ++p) {
+      float* v = sum + p * E;
+      if (VECTOR) {
+        if (col(p, 0) >= hidden) continue;
+        TO* q = row + col(p, 0);
+        float w[E];
+        if constexpr (E * sizeof(TO) % 16 == 0) {
+          if (add) rows::load_vec<TO, E>(q, w);
+        } else if (add) {                   // fp32 rows into bf16: 8 bytes
+          const uint2 u = *reinterpret_cast<const uint2*>(q);
+          w[0] = __uint_as_float(u.x << 16); w[1] = __uint_as_float(u.x & 0xffff0000u);
+          w[2] = __uint_as_float(u.y << 16); w[3] = __uint_as_float(u.y & 0xffff0000u);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = add ? fmaf(scale, v[e], old[e]) : scale * v[e];
-        const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
-        *q = make_uint2(*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b));
-      }
-    } else {
+        for (int e = 0; e < E; ++e) w[e] = add ? fmaf(scale, v[e], w[e]) : scale * v[e];
+        if constexpr (E * sizeof(TO) % 16 == 0) {
+          rows::store_vec<TO, E>(q, w);
+        } else {
+          static_assert(E == 4 && sizeof(TO) == 2, "");
+          const __nv_bfloat162 a = __floats2bfloat162_rn(w[0], w[1]), b = __floats2bfloat162_rn(w[2], w[3]);
+          *reinterpret_cast<uint2*>(q) = make_uint2(*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b));
+        }
+      } else {
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const int c = col0 + e * 32 + lane;
-        if (c < hidden) row[c] = from_float<TO>(add ? fmaf(scale, v[e], to_float<TO>(row[c])) : scale * v[e]);
+        for (int e = 0; e < E; ++e) {
+          const int c = col(p, e);
+          if (c < hidden) row[c] = from_float<TO>(add ? fmaf(scale, v[e], to_float<TO>(row[c])) : scale * v[e]);
+        }
       }
     }
   }
-  // A part of a long row: 32 N floats, of which a lane keeps its own.
+  // A part of a long row: WIDTH floats, of which a lane keeps its own.
   __device__ __forceinline__ void store_part(float* p, const float (&v)[N]) const {
 #pragma unroll
     for (int e = 0; e < N; e += 4) __stcg(reinterpret_cast<float4*>(p + e * 32) + lane, make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]));
@@ -270,47 +320,76 @@ struct Slice {
   }
 };
 
-template <typename TI, typename TO, bool VECTOR>
-__global__ void __launch_bounds__(EM_THREADS)
-k_table_grad(const int2* order, const int* start, unsigned* counters, float* parts,
-             const TI* __restrict__ dY, long long ld, int vocab, int hidden, int T, long long chunks, int slices, float scale, int add,
-             TO* __restrict__ G, long long ldg) {
-  constexpr int N = rows::PER16<TI>;
-  const int lane = threadIdx.x & 31;
-  const long long unit = (long long)blockIdx.x * EM_WARPS + (threadIdx.x >> 5);
-  ptx::grid_wait();
-  if (unit >= chunks * slices) {            // rows that no token names
-    const long long first = (unit - chunks * slices) * TG_ZERO_ROWS;
-    if (add || first >= vocab) return;     // (the last block has warps to spare)
-    const int here = (int)min((long long)TG_ZERO_ROWS, vocab - first);
-    const int s = lane <= here ? start[first + lane] : 0;
-    const int next = __shfl_down_sync(0xffffffffu, s, 1);     // (by all lanes)
-    const unsigned empty = __ballot_sync(0xffffffffu, lane < here && s == next);
-    for (int k = 0; k < here; ++k) {
-      if (!(empty >> k & 1)) continue;
-      TO* row = G + (first + k) * ldg;
-      if (VECTOR) {
-        const int bytes = hidden * (int)sizeof(TO);     // a multiple of 8
-        for (int b = lane * 8; b < bytes; b += 256) *reinterpret_cast<uint2*>(reinterpret_cast<char*>(row) + b) = make_uint2(0u, 0u);
-      } else {
-        for (int c = lane; c < hidden; c += 32) row[c] = from_float<TO>(0.f);
-      }
+// Zeroes the rows of `first` on that no token names.  early: in front of the wait for k_token_order, from the tokens.
+template <typename TO, typename TOK, bool VECTOR>
+__device__ __forceinline__ void zero_rows(long long first, int vocab, int hidden, const int2* span, const TOK* __restrict__ tokens, int n, bool early, TO* G,
+                                          long long ldg) {
+  __shared__ unsigned char named[TG_ZERO_ROWS];
+  const int here = (int)min((long long)TG_ZERO_ROWS, vocab - first);
+  if (early) {
+    for (int k = threadIdx.x; k < TG_ZERO_ROWS; k += EM_THREADS) named[k] = 0;
+    __syncthreads();
+#pragma unroll 8
+    for (int i = threadIdx.x; i < n; i += EM_THREADS) {
+      const long long r = (long long)tokens[i] - first;
+      if (r >= 0 && r < here) named[r] = 1;
     }
+  } else {
+    ptx::grid_wait();
+    for (int k = threadIdx.x; k < here; k += EM_THREADS) {
+      const int2 s = span[first + k];
+      named[k] = s.x != s.y;
+    }
+  }
+  __syncthreads();
+  const int lane = threadIdx.x & 31;
+  for (int k = threadIdx.x >> 5; k < here; k += EM_WARPS) {
+    if (named[k]) continue;
+    TO* row = G + (first + k) * ldg;
+    if (VECTOR) {
+      const int bytes = hidden * (int)sizeof(TO);       // a multiple of 8
+      for (int b = lane * 16; b + 16 <= bytes; b += 512) *reinterpret_cast<uint4*>(reinterpret_cast<char*>(row) + b) = make_uint4(0u, 0u, 0u, 0u);
+      if (lane == 0 && (bytes & 8)) *reinterpret_cast<uint2*>(reinterpret_cast<char*>(row) + bytes - 8) = make_uint2(0u, 0u);
+    } else {
+      for (int c = lane; c < hidden; c += 32) row[c] = from_float<TO>(0.f);
+    }
+  }
+}
+
+// zero_blocks blocks zero, TG_ZERO_ROWS rows each; the warps of the others take a stretch of T positions and a slice each.
+template <typename TI, typename TO, typename TOK, bool VECTOR, int PIECES>
+__global__ void __launch_bounds__(EM_THREADS, PIECES == 1 ? 4 : 3)
+k_table_grad(const int2* order, const int2* span, const int* total, unsigned* counters, float* parts, const TOK* __restrict__ tokens, int ntokens,
+             const TI* __restrict__ dY, long long ld, int vocab, int hidden, long long chunks, int slices, int zero_blocks, float scale, int add,
+             TO* __restrict__ G, long long ldg) {
+  using Cols = Slice<TI, TO, VECTOR, PIECES>;
+  constexpr int N = Cols::N;
+  __shared__ uint4 ring[EM_WARPS][TG_DEPTH][32 * PIECES];
+  // blocks that zero: in front where they need not wait, behind (where they fill the places that others leave) otherwise
+  const bool early = ntokens <= TG_ZERO_EARLY;
+  const int main_blocks = gridDim.x - zero_blocks, block = early ? (int)blockIdx.x - zero_blocks : (int)blockIdx.x;
+  if (block < 0 || block >= main_blocks) {
+    zero_rows<TO, TOK, VECTOR>((long long)(early ? blockIdx.x : block - main_blocks) * TG_ZERO_ROWS, vocab, hidden, span, tokens, ntokens, early, G, ldg);
+    ptx::grid_wait();                       // (this kernel does not end before the one in front of it)
     return;
   }
+  const int lane = threadIdx.x & 31;
+  const long long unit = (long long)block * EM_WARPS + (threadIdx.x >> 5);
+  ptx::grid_wait();
   const long long chunk = unit / slices;
-  const int slice = (int)(unit % slices);
-  const int n = start[vocab];
+  const int slice = (int)(unit - chunk * slices);
+  const int n = *total;
+  const int T = max(TG_MIN, (int)((n + chunks - 1) / chunks));
   const long long p0 = chunk * T;
-  if (p0 >= n) return;
+  if (chunk >= chunks || p0 >= n) return;
   const int a0 = (int)p0, p1 = (int)min(p0 + T, (long long)n);
   const int v_first = order[a0].y, v_last = order[p1 - 1].y;
-  const int first_s = start[v_first], first_e = start[v_first + 1], last_s = start[v_last], last_e = start[v_last + 1];
+  const int2 sf = span[v_first], sl = span[v_last];
+  const int first_s = sf.x, first_e = sf.y, last_s = sl.x, last_e = sl.y;
   const bool first_long = first_e - first_s > T, last_long = last_e - last_s > T;
   const int a = !first_long && first_s < a0 ? first_e : a0, b = last_long ? p1 : last_e;
   if (a >= b) return;
-  Slice<TI, TO, VECTOR> at;
-  at.col0 = slice * 32 * N; at.lane = lane; at.hidden = hidden;
+  const Cols at{slice * Cols::WIDTH, lane, hidden};
 
   float sum[N];
 #pragma unroll
@@ -323,7 +402,7 @@ k_table_grad(const int2* order, const int* start, unsigned* counters, float* par
       const int s = v == v_first ? first_s : last_s, e = v == v_first ? first_e : last_e;
       const long long c0 = s / T, c1 = (e - 1) / T;
       // two long rows may meet in a chunk: the one that begins there has the second place
-      auto part = [&](long long c) { return parts + ((2 * c + (c == c0 ? 1 : 0)) * slices + slice) * (32 * N); };
+      auto part = [&](long long c) { return parts + ((2 * c + (c == c0 ? 1 : 0)) * slices + slice) * Cols::WIDTH; };
       at.store_part(part(chunk), sum);
       __threadfence();
       __syncwarp();
@@ -342,27 +421,49 @@ k_table_grad(const int2* order, const int* start, unsigned* counters, float* par
 #pragma unroll
     for (int k = 0; k < N; ++k) sum[k] = 0.f;
   };
-  int current = order[a].y;
+  // A window of 32 positions of the order: their tokens, and the rows that are fetched while they are summed.
+  uint4 (*slots)[32 * PIECES] = ring[threadIdx.x >> 5];
+  auto token_at = [&](int k) { return k < b ? order[k].y : -1; };
+  auto row_at = [&](int k) { return k < b ? order[k].x : -1; };
+  const int ahead = row_at(a + lane);
+  int token = token_at(a + lane), row = row_at(a + TG_DEPTH + lane);
+#pragma unroll
+  for (int k = 0; k < TG_DEPTH; ++k) {
+    const int i = __shfl_sync(0xffffffffu, ahead, k);
+    if (i >= 0) at.fetch(dY + (long long)i * ld, slots[k]);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  int current = __shfl_sync(0xffffffffu, token, 0);
   for (int q = a; q < b; q += 32) {
-    const int2 entry = q + lane < b ? order[q + lane] : make_int2(0, 0);
+    const int token_next = token_at(q + 32 + lane), row_next = row_at(q + 32 + TG_DEPTH + lane);
     const int m = min(32, b - q);
-    for (int k = 0; k < m; k += TG_UNROLL) {
-      typename Slice<TI, TO, VECTOR>::Piece v[TG_UNROLL];
-#pragma unroll
-      for (int u = 0; u < TG_UNROLL; ++u) {
-        *reinterpret_cast<uint4*>(&v[u]) = make_uint4(0u, 0u, 0u, 0u);
-        const int i = __shfl_sync(0xffffffffu, entry.x, (k + u) & 31);
-        if (k + u < m) at.load(dY + (long long)i * ld, v[u]);
+    const int before = __shfl_up_sync(0xffffffffu, token, 1);
+    const unsigned changes = __ballot_sync(0xffffffffu, token != (lane ? before : current));     // where another row begins
+    int k = 0;
+    while (true) {
+      const unsigned rest = changes >> k;               // (k < 32)
+      const int end = rest ? min(m, k + __ffs(rest) - 1) : m;
+      for (; k < end; ++k) {
+        asm volatile("cp.async.wait_group %0;" :: "n"(TG_DEPTH - 1) : "memory");
+        uint4* slot = slots[k % TG_DEPTH];
+        at.add(slot, sum);
+        const int i = __shfl_sync(0xffffffffu, row, k);
+        if (i >= 0) at.fetch(dY + (long long)i * ld, slot);
+        asm volatile("cp.async.commit_group;" ::: "memory");
       }
-#pragma unroll
-      for (int u = 0; u < TG_UNROLL; ++u) {
-        const int t = __shfl_sync(0xffffffffu, entry.y, (k + u) & 31);
-        if (k + u < m) {
-          if (t != current) { flush(current); current = t; }
-          at.add(v[u], sum);
-        }
-      }
+      if (k >= m) break;
+      flush(current);
+      current = __shfl_sync(0xffffffffu, token, k);
+      // the position that began it is summed now; the next change is looked for behind it
+      asm volatile("cp.async.wait_group %0;" :: "n"(TG_DEPTH - 1) : "memory");
+      uint4* slot = slots[k % TG_DEPTH];
+      at.add(slot, sum);
+      const int i = __shfl_sync(0xffffffffu, row, k);
+      if (i >= 0) at.fetch(dY + (long long)i * ld, slot);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      if (++k >= m) break;
     }
+    token = token_next; row = row_next;
   }
   flush(current);
 }
@@ -370,16 +471,24 @@ k_table_grad(const int2* order, const int* start, unsigned* counters, float* par
 // The grid and the sections of the workspace of a gradient.
 TablePlan plan_for(long long n, long long vocab, long long hidden, bool f32) {
   TablePlan p;
-  p.range = (int)std::min<long long>(ORD_MAX_ROWS, std::max<long long>(32, (vocab + EM_SMS - 1) / EM_SMS));
-  p.blocks = (int)((vocab + p.range - 1) / p.range);
-  const long long width = 32 * (f32 ? 4 : 8);
+  p.blocks = ORD_MIN_BLOCKS;
+  while ((vocab + p.blocks - 1) / p.blocks > ORD_MAX_ROWS) p.blocks *= 2;
+  p.shift = 0;
+  while ((1 << p.shift) < p.blocks) ++p.shift;
+  p.nrows = (int)((vocab + p.blocks - 1) / p.blocks);
+  // every warp has counts of its own, which cost time per warp: few warps for few tokens
+  p.threads = n > 32768 ? ORD_MAX_THREADS : n > 8192 ? 512 : 256;
+  // 512 bytes of dY per warp and row, or 1024, which takes fewer instructions per byte
+  p.pieces = hidden > 32 * (f32 ? 4 : 8) ? 2 : 1;
+  const long long width = 32 * (f32 ? 4 : 8) * p.pieces;
   p.slices = (int)((hidden + width - 1) / width);
-  // Few positions: short stretches, so that all SMs have warps enough; many: long ones, whose parts of long rows weigh little.
-  p.T = 16;
-  while (p.T < 128 && (n / (2 * p.T)) * p.slices >= EM_SMS * 32) p.T *= 2;
-  p.chunks = (n + p.T - 1) / p.T;
+  // As many stretches as there are warps on the GPU at once, all of one length, which follows from the number of tokens
+  // that the device finds; of few positions as many as have TG_MIN each.
+  p.chunks = std::max<long long>(1, std::min<long long>((n + TG_MIN - 1) / TG_MIN, EM_SMS * (p.pieces == 2 ? 3 : 4) * EM_WARPS / p.slices));
+  if (n == 0) p.chunks = 0;
   size_t at = align_up((size_t)n * sizeof(int2));
-  p.off_start = at; at += align_up((size_t)(vocab + 1) * sizeof(int));
+  p.off_span = at; at += align_up((size_t)vocab * sizeof(int2));
+  p.off_total = at; at += 256;
   p.off_counters = at; at += align_up((size_t)p.chunks * p.slices * sizeof(unsigned));
   p.off_parts = at; at += (size_t)p.chunks * 2 * p.slices * width * sizeof(float);
   p.bytes = align_up(std::max<size_t>(at, 256));
@@ -408,28 +517,32 @@ void run_lookup(const void* table, long long ld, const void* tokens, long long n
     k_embedding<T, TOK, false><<<blocks, EM_THREADS, 0, st>>>((const T*)table, ld, (const TOK*)tokens, n, vocab, hidden, slices, scale, (T*)out, ld_out);
 }
 
-// The counts of a block's range are above the default limit of shared memory: a setting per device and kernel.
+// Counts and lists may be above the default limit of shared memory: a setting per device and kernel.
 template <typename TOK, bool VECTOR>
 cudaError_t run_order(const TablePlan& p, const void* tokens, int n, int vocab, char* work, cudaStream_t st) {
-  const size_t smem = (size_t)ORD_WARPS * p.range * sizeof(unsigned);
-  if (smem > 48 * 1024 - 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(k_token_order<TOK, VECTOR>, cudaFuncAttributeMaxDynamicSharedMemorySize, ORD_WARPS * ORD_MAX_ROWS * 4);
+  auto bytes = [](int warps, int nrows) { return (size_t)((warps * nrows + 1) & ~1) * sizeof(unsigned) + (size_t)warps * ORD_LIST * sizeof(int2); };
+  const size_t smem = bytes(p.threads / 32, p.nrows);
+  if (smem > 47 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(k_token_order<TOK, VECTOR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes(ORD_MAX_THREADS / 32, ORD_MAX_ROWS));
     if (e != cudaSuccess) return e;
   }
-  k_token_order<TOK, VECTOR><<<p.blocks, ORD_THREADS, smem, st>>>((const TOK*)tokens, n, vocab, p.range, (int2*)work, (int*)(work + p.off_start),
-                                                                  (unsigned*)(work + p.off_counters), p.chunks * p.slices);
+  k_token_order<TOK, VECTOR><<<p.blocks, p.threads, smem, st>>>((const TOK*)tokens, n, vocab, p.shift, p.nrows, (int2*)work, (int2*)(work + p.off_span),
+                                                                (int*)(work + p.off_total), (unsigned*)(work + p.off_counters), p.chunks * p.slices);
   return cudaGetLastError();
 }
 
-template <typename TI, typename TO>
-cudaError_t run_grad(const TablePlan& p, const void* dY, long long ld, int vocab, int hidden, float scale, int add, void* G, long long ldg, char* work,
+template <typename TI, typename TO, typename TOK>
+cudaError_t run_grad(const TablePlan& p, const void* tokens, int n, const void* dY, long long ld, int vocab, int hidden, float scale, int add, void* G, long long ldg, char* work,
                      bool vector, cudaStream_t st) {
-  const long long units = p.chunks * p.slices + (add ? 0 : (vocab + TG_ZERO_ROWS - 1) / TG_ZERO_ROWS);
-  if (units == 0) return cudaSuccess;
-  const dim3 grid((unsigned)((units + EM_WARPS - 1) / EM_WARPS));
-  return launch_chained(vector ? k_table_grad<TI, TO, true> : k_table_grad<TI, TO, false>, grid, EM_THREADS, 0, st, true, 1, (const int2*)work,
-                        (const int*)(work + p.off_start), (unsigned*)(work + p.off_counters), (float*)(work + p.off_parts), (const TI*)dY, ld,
-                        vocab, hidden, p.T, p.chunks, p.slices, scale, add, (TO*)G, ldg);
+  const int zero_blocks = add ? 0 : (vocab + TG_ZERO_ROWS - 1) / TG_ZERO_ROWS;
+  const dim3 grid((unsigned)(zero_blocks + (p.chunks * p.slices + EM_WARPS - 1) / EM_WARPS));
+  if (grid.x == 0) return cudaSuccess;
+  auto kernel = p.pieces == 2 ? (vector ? k_table_grad<TI, TO, TOK, true, 2> : k_table_grad<TI, TO, TOK, false, 2>)
+                              : (vector ? k_table_grad<TI, TO, TOK, true, 1> : k_table_grad<TI, TO, TOK, false, 1>);
+  return launch_chained(kernel, grid, EM_THREADS, 0, st, true, 1, (const int2*)work,
+                        (const int2*)(work + p.off_span), (const int*)(work + p.off_total), (unsigned*)(work + p.off_counters),
+                        (float*)(work + p.off_parts), (const TOK*)tokens, n, (const TI*)dY, ld, vocab, hidden, p.chunks, p.slices, zero_blocks, scale,
+                        add, (TO*)G, ldg);
 }
 
 }  // namespace
@@ -505,14 +618,14 @@ extern "C" fira_status fira_embedding_grad(const void* tokens_dev, int32_t token
     else e = token_vector ? run_order<long long, true>(p, tokens_dev, n, v, work, st) : run_order<long long, false>(p, tokens_dev, n, v, work, st);
     // a lane's piece of dY is 16 bytes; of G it is 8, 16 or 32
     const bool vector = rows::aligned16(dY_dev, ld, hidden, es) && (ldg * (long long)gs) % 16 == 0 && ((uintptr_t)G_dev & 15) == 0;
+#define EM_GRAD(TI, TO)                                                                                                          \
+  (token_bits == 32 ? run_grad<TI, TO, int>(p, tokens_dev, n, dY_dev, ld, v, h, scale, accumulate != 0, G_dev, ldg, work, vector, st) \
+                    : run_grad<TI, TO, long long>(p, tokens_dev, n, dY_dev, ld, v, h, scale, accumulate != 0, G_dev, ldg, work, vector, st))
     if (e == cudaSuccess) {
-      if (dtype == FIRA_BF16)
-        e = grad_dtype == FIRA_BF16 ? run_grad<__nv_bfloat16, __nv_bfloat16>(p, dY_dev, ld, v, h, scale, accumulate != 0, G_dev, ldg, work, vector, st)
-                                    : run_grad<__nv_bfloat16, float>(p, dY_dev, ld, v, h, scale, accumulate != 0, G_dev, ldg, work, vector, st);
-      else
-        e = grad_dtype == FIRA_BF16 ? run_grad<float, __nv_bfloat16>(p, dY_dev, ld, v, h, scale, accumulate != 0, G_dev, ldg, work, vector, st)
-                                    : run_grad<float, float>(p, dY_dev, ld, v, h, scale, accumulate != 0, G_dev, ldg, work, vector, st);
+      if (dtype == FIRA_BF16) e = grad_dtype == FIRA_BF16 ? EM_GRAD(__nv_bfloat16, __nv_bfloat16) : EM_GRAD(__nv_bfloat16, float);
+      else e = grad_dtype == FIRA_BF16 ? EM_GRAD(float, __nv_bfloat16) : EM_GRAD(float, float);
     }
+#undef EM_GRAD
     if (e != cudaSuccess) { set_error(who + ": " + cudaGetErrorString(e)); return FIRA_ERR_CUDA; }
     return FIRA_OK;
   });

@@ -23,6 +23,14 @@ __device__ __forceinline__ void unpack(const uint4& u, float* v) {
     }
   }
 }
+// Two fp32 additions in one instruction.
+__device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
+  asm("{ .reg .b64 p, q;\n\t"
+      "mov.b64 p, {%0, %1};\n\t"
+      "mov.b64 q, {%2, %3};\n\t"
+      "add.rn.f32x2 p, p, q;\n\t"
+      "mov.b64 {%0, %1}, p; }" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
 template <typename T, int N>
 __device__ __forceinline__ void load_vec(const T* p, float (&v)[N]) {
   static_assert(N % PER16<T> == 0, "whole 16-byte accesses");
