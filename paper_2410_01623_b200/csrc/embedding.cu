@@ -267,10 +267,13 @@ struct Slice {
   __device__ __forceinline__ void add(const uint4* slot, float (&sum)[N]) const {
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-      float v[E];
+      float2 v[E / 2];
       rows::unpack<TI>(slot[p * 32 + lane], v);         // (columns beyond the width: whatever is there, never stored)
 #pragma unroll
-      for (int e = 0; e < E; e += 2) rows::add2(sum[p * E + e], sum[p * E + e + 1], v[e], v[e + 1]);
+      for (int e = 0; e < E; e += 2) {
+        const float2 s = rows::add2(make_float2(sum[p * E + e], sum[p * E + e + 1]), v[e / 2]);
+        sum[p * E + e] = s.x; sum[p * E + e + 1] = s.y;
+      }
     }
   }
   __device__ __forceinline__ void store(TO* row, float (&sum)[N], float scale, bool add) const {

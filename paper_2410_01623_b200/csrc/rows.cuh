@@ -23,13 +23,42 @@ __device__ __forceinline__ void unpack(const uint4& u, float* v) {
     }
   }
 }
-// Two fp32 additions in one instruction.
-__device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
-  asm("{ .reg .b64 p, q;\n\t"
-      "mov.b64 p, {%0, %1};\n\t"
-      "mov.b64 q, {%2, %3};\n\t"
-      "add.rn.f32x2 p, p, q;\n\t"
-      "mov.b64 {%0, %1}, p; }" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+// Two fp32 operations in one instruction, each rounded like the single one.
+__device__ __forceinline__ unsigned long long bits2(float2 v) { return *reinterpret_cast<const unsigned long long*>(&v); }
+__device__ __forceinline__ float2 from_bits2(unsigned long long b) { return *reinterpret_cast<const float2*>(&b); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  unsigned long long d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)));
+  return from_bits2(d);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  unsigned long long d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)));
+  return from_bits2(d);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+  return from_bits2(d);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// The elements of 16 bytes in pairs, and back (rounded).
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4& u, float2 (&v)[PER16<T> / 2]) { unpack<T>(u, &v[0].x); }
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float2 (&v)[PER16<T> / 2]) {
+  unsigned w[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if constexpr (sizeof(T) == 4) {
+      w[k] = __float_as_uint(k & 1 ? v[k / 2].y : v[k / 2].x);
+    } else {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(v[k].x, v[k].y);
+      w[k] = *reinterpret_cast<const unsigned*>(&h);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 template <typename T, int N>
 __device__ __forceinline__ void load_vec(const T* p, float (&v)[N]) {
