@@ -7,7 +7,6 @@ library is missing, `lib()` raises; there is no fallback.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import os
 from array import array
@@ -98,10 +97,10 @@ SIGNATURES = {
                                   C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.POINTER(C.c_int64), C.c_int,
                                   C.c_int64, C.c_float, C.c_void_p]),
     "fira_grad_work_bytes": (C.c_size_t, [C.c_int32]),
-    "fira_grad_norm": (C.c_int, [C.c_int32, C.POINTER(GradDesc), C.POINTER(C.c_void_p), C.c_void_p, C.c_void_p,
-                                 C.c_size_t, C.c_void_p]),
-    "fira_clip_grads": (C.c_int, [C.c_int32, C.POINTER(GradDesc), C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
-                                  C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    # (host arrays by address: GradDesc and device pointers)
+    "fira_grad_norm": (C.c_int, [C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "fira_clip_grads": (C.c_int, [C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p,
+                                  C.c_void_p, C.c_size_t, C.c_void_p]),
     "fira_embedding": (C.c_int, [C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int, C.c_void_p, C.c_int32, C.c_int64,
                                  C.c_float, C.c_void_p, C.c_int64, C.c_void_p]),
     "fira_embedding_grad_work_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64, C.c_int]),
@@ -175,30 +174,48 @@ def adam_dense(hp: Hparams, Ws: Sequence[torch.Tensor], Gs: Sequence[torch.Tenso
 
 
 _CODES = {torch.float32: FIRA_F32, torch.bfloat16: FIRA_BF16}
+_TOKEN_BITS = {torch.int32: 32, torch.int64: 64}
+_T = torch.Tensor
+
+# The stream's address by itself (0.1 us instead of 3, where a small call takes 10 in all).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _refuse(what: str):
+    raise ValueError(what)
 
 
 def _code(t: torch.Tensor, what: str) -> int:
     code = _CODES.get(t.dtype)
-    if code is None:
-        raise ValueError(f"{what}: float32 or bfloat16, not {t.dtype}")
-    return code
+    return _refuse(f"{what}: float32 or bfloat16, not {t.dtype}") if code is None else code
 
 
-@contextlib.contextmanager
-def _other_device(device):
-    with torch.cuda.device(device):
-        yield
+def _device_of(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
+    """The index of the CUDA device that all of a call's tensors lie on."""
+    index = first.get_device()
+    if index < 0:
+        raise ValueError(f"the Fira library runs on a CUDA device only, not on {first.device}")
+    for t in others:
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"tensors on {t.device} and on {first.device}")
+    return index
 
 
-def _on(device: torch.device):
-    """The device whose tensors a call gets, as the current one (torch.cuda.device costs a few microseconds, which a
-    call on the current device need not pay)."""
-    if device.type != "cuda":
-        raise ValueError(f"the Fira library runs on a CUDA device only, not on {device}")
-    return _HERE if device.index == torch.cuda.current_device() else _other_device(device)
+def _pitch(t: torch.Tensor, what: str) -> int:
+    """Elements from row to row of a tensor whose last dimension is a row."""
+    if t.is_contiguous():
+        return 0
+    if t.dim() == 2 and (t.shape[1] == 1 or t.stride(1) == 1) and (t.shape[0] == 1 or t.stride(0) >= t.shape[1]):
+        return t.stride(0) if t.shape[0] > 1 else 0
+    raise ValueError(f"{what}: strides {tuple(t.stride())} of shape {tuple(t.shape)}: rows of one pitch are needed")
 
 
-_HERE = contextlib.nullcontext()
+def _rows_or_copy(t: torch.Tensor) -> torch.Tensor:
+    """t, or its rows one behind another where they have no one pitch."""
+    if t.is_contiguous() or (t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]):
+        return t
+    return t.contiguous()
 
 
 def _rows(t: torch.Tensor, flip: bool):
@@ -230,28 +247,29 @@ def _grad_codes(tensors: Sequence[torch.Tensor]):
     if not types <= _CODES.keys():
         raise ValueError(f"gradients and their outputs are float32 or bfloat16, not {types}")
     if len(types) == 1:
-        return array("i", [_CODES[types.pop()]]) * len(tensors)
+        return array("i", (_CODES[types.pop()],)) * len(tensors)
     return array("i", [_CODES[t.dtype] for t in tensors])
 
 
 def _grad_list(Gs: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]]):
-    """The descriptors and pointers of a list of gradients.  Whole lists go through map() and arrays: a fifth of the
-    time that a loop over the tensors takes (a small list is bound by it)."""
+    """The device's index and the arrays that go to the library: descriptors, addresses, the outputs' addresses.  Whole
+    lists go through map() and arrays: a small list is bound by this."""
     n = len(Gs)
     if n == 0:
         raise ValueError("an empty list of gradients")
-    T = torch.Tensor
     outs = Gs if out is None else out
-    device = Gs[0].device
     codes = _grad_codes(Gs)
     out_codes = codes if out is None else _grad_codes(out)
-    if len(set(map(T.get_device, Gs)).union(() if out is None else map(T.get_device, out))) > 1:
+    devices = set(map(_T.get_device, Gs))
+    if out is not None:
+        devices.update(map(_T.get_device, out))
+    if len(devices) > 1:
         raise ValueError("the gradients and their outputs lie on different devices")
     words = array("q", bytes(40 * n))
-    if all(map(T.is_contiguous, Gs)) and (out is None or (all(map(T.is_contiguous, out)) and
-                                                          [g.shape for g in Gs] == [o.shape for o in out])):
-        words[0::5] = array("q", [1]) * n
-        words[1::5] = array("q", map(T.numel, Gs))
+    if all(map(_T.is_contiguous, Gs)) and (out is None or (all(map(_T.is_contiguous, out)) and
+                                                           [g.shape for g in Gs] == [o.shape for o in out])):
+        words[0::5] = array("q", (1,)) * n
+        words[1::5] = array("q", map(_T.numel, Gs))
     else:
         flat = [w for i, (g, o) in enumerate(zip(Gs, outs)) for w in _grad_words(i, g, o)]
         for k in range(4):
@@ -259,23 +277,34 @@ def _grad_list(Gs: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]]
     both = array("i", bytes(8 * n))
     both[0::2], both[1::2] = codes, out_codes
     words[4::5] = array("q", both.tobytes())
-    pointers = C.c_void_p * n
-    return (device, n, (GradDesc * n).from_buffer(words), pointers.from_buffer(array("Q", map(T.data_ptr, Gs))),
-            None if out is None else pointers.from_buffer(array("Q", map(T.data_ptr, out))))
+    index = devices.pop()
+    if index < 0:
+        raise ValueError(f"the Fira library runs on a CUDA device only, not on {Gs[0].device}")
+    return index, words, array("Q", map(_T.data_ptr, Gs)), None if out is None else array("Q", map(_T.data_ptr, out))
+
+
+def grad_work_bytes(count: int) -> int:
+    return lib().fira_grad_work_bytes(count)
 
 
 def grad_norm(Gs: Sequence[torch.Tensor], work: Optional[torch.Tensor] = None) -> torch.Tensor:
     """fira_grad_norm: the norm over all elements of a list of gradients (float32 and bfloat16 may be mixed), as a
     float32 tensor of one element on the device; nothing waits for it.  work: a byte tensor of at least
     grad_work_bytes(len(Gs)) bytes; by default torch's allocator lends one for the call."""
-    device, n, descs, ptrs, _ = _grad_list(Gs, None)
-    with _on(device):
-        nbytes = lib().fira_grad_work_bytes(n)
-        if work is None:
-            work = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        norm = torch.empty((), dtype=torch.float32, device=device)
-        check(lib().fira_grad_norm(n, descs, ptrs, norm.data_ptr(), work.data_ptr(), work.numel() * work.element_size(),
-                                   torch.cuda.current_stream().cuda_stream))
+    index, words, at, _ = _grad_list(Gs, None)
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return grad_norm(Gs, work)
+    L, n, device = lib(), len(Gs), Gs[0].device
+    if work is None:
+        work = torch.empty(L.fira_grad_work_bytes(n), dtype=torch.uint8, device=device)
+    elif work.get_device() != index:
+        raise ValueError(f"work is on {work.device}, the gradients on {device}")
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    status = L.fira_grad_norm(n, words.buffer_info()[0], at.buffer_info()[0], norm.data_ptr(), work.data_ptr(),
+                              work.nbytes, _raw_stream(index))
+    if status:
+        check(status)
     return norm
 
 
@@ -283,71 +312,52 @@ def clip_grads(Gs: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequen
                work: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """fira_clip_grads: scales a list of gradients so that their global norm is at most max_norm, in place or into `out`
     (tensors of the same shapes, float32 or bfloat16 each), and returns the norm before it and the factor, as float32
-    tensors of one element on the device."""
+    tensors of one element on the device.  work: as for grad_norm."""
     if out is not None and len(out) != len(Gs):
         raise ValueError(f"{len(out)} outputs for {len(Gs)} gradients")
-    device, n, descs, ptrs, out_ptrs = _grad_list(Gs, out)
-    with _on(device):
-        if work is None:
-            work = torch.empty(lib().fira_grad_work_bytes(n), dtype=torch.uint8, device=device)
-        norm, scale = torch.empty(2, dtype=torch.float32, device=device).unbind()
-        check(lib().fira_clip_grads(n, descs, ptrs, out_ptrs, max_norm, norm.data_ptr(), scale.data_ptr(), work.data_ptr(),
-                                    work.numel() * work.element_size(), torch.cuda.current_stream().cuda_stream))
+    index, words, at, out_at = _grad_list(Gs, out)
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return clip_grads(Gs, max_norm, out, work)
+    L, n, device = lib(), len(Gs), Gs[0].device
+    if work is None:
+        work = torch.empty(L.fira_grad_work_bytes(n), dtype=torch.uint8, device=device)
+    elif work.get_device() != index:
+        raise ValueError(f"work is on {work.device}, the gradients on {device}")
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    scale = torch.empty_like(norm)
+    status = L.fira_clip_grads(n, words.buffer_info()[0], at.buffer_info()[0],
+                               None if out_at is None else out_at.buffer_info()[0], max_norm, norm.data_ptr(),
+                               scale.data_ptr(), work.data_ptr(), work.nbytes, _raw_stream(index))
+    if status:
+        check(status)
     return norm, scale
-
-
-def grad_work_bytes(count: int) -> int:
-    return lib().fira_grad_work_bytes(count)
-
-
-_TOKEN_BITS = {torch.int32: 32, torch.int64: 64}
-
-
-def _token_bits(tokens: torch.Tensor) -> int:
-    bits = _TOKEN_BITS.get(tokens.dtype)
-    if bits is None:
-        raise ValueError(f"tokens are int32 or int64, not {tokens.dtype}")
-    return bits
-
-
-def _pitch(t: torch.Tensor, what: str) -> int:
-    """Elements from row to row of a tensor whose last dimension is a row."""
-    if t.is_contiguous():
-        return t.shape[-1]
-    if t.dim() == 2 and (t.shape[1] == 1 or t.stride(1) == 1) and (t.shape[0] == 1 or t.stride(0) >= t.shape[1]):
-        return t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    raise ValueError(f"{what}: strides {tuple(t.stride())} of shape {tuple(t.shape)}: rows of one pitch are needed")
-
-
-def _address(t: torch.Tensor):
-    """A tensor's address; of an empty one, which has none, one that is not NULL and that nothing is read from."""
-    return t.data_ptr() or 256
-
-
-def _same_device(device: torch.device, **tensors: Optional[torch.Tensor]) -> None:
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, not on {device}")
 
 
 def embedding(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0,
               out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """fira_embedding: scale * table[tokens] (shape of tokens + (hidden,)); zeros where a token is not in 0 .. vocab-1."""
-    code, bits = _code(table, "table"), _token_bits(tokens)
-    if table.dim() != 2 or table.shape[0] == 0 or table.shape[1] == 0:
+    code = _code(table, "table")
+    bits = _TOKEN_BITS.get(tokens.dtype) or _refuse(f"tokens are int32 or int64, not {tokens.dtype}")
+    if table.dim() != 2 or table.numel() == 0:
         raise ValueError(f"the table is a matrix, not {tuple(table.shape)}")
-    device, (vocab, hidden) = table.device, table.shape
-    shape = (*tokens.shape, hidden)
-    _same_device(device, tokens=tokens, out=out)
+    vocab, hidden = table.shape
     ld = _pitch(table, "table")
-    with _on(device):
-        tokens = tokens.contiguous()
-        if out is None:
-            out = torch.empty(shape, dtype=table.dtype, device=device)
-        elif out.shape != shape or out.dtype != table.dtype:
-            raise ValueError(f"out: {shape} of {table.dtype} is needed, not {tuple(out.shape)} of {out.dtype}")
-        check(lib().fira_embedding(table.data_ptr(), vocab, hidden, ld, code, tokens.data_ptr(), bits, tokens.numel(),
-                                   scale, out.data_ptr(), _pitch(out, "out"), torch.cuda.current_stream().cuda_stream))
+    index = _device_of(table, tokens, out)
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return embedding(table, tokens, scale, out)
+    tokens = tokens.contiguous()
+    if out is None:
+        out, ld_out = table.new_empty((*tokens.shape, hidden)), 0
+    elif out.shape != (*tokens.shape, hidden) or out.dtype != table.dtype:
+        raise ValueError(f"out: {(*tokens.shape, hidden)} of {table.dtype} is needed, not {tuple(out.shape)} of {out.dtype}")
+    else:
+        ld_out = _pitch(out, "out")
+    status = lib().fira_embedding(table.data_ptr(), vocab, hidden, ld, code, tokens.data_ptr(), bits, tokens.numel(), scale,
+                                  out.data_ptr(), ld_out, _raw_stream(index))
+    if status:
+        check(status)
     return out
 
 
@@ -357,35 +367,37 @@ def embedding_grad(tokens: torch.Tensor, dY: torch.Tensor, vocab: int, scale: fl
     """fira_embedding_grad: the gradient (vocab, hidden) of the table from that of scale * table[tokens].  out: float32 or
     bfloat16, by default a new tensor of dY's type; accumulate: added to what is in it.  work: a byte tensor of at least
     lib().fira_embedding_grad_work_bytes() bytes; by default torch's allocator lends one for the call."""
-    code, bits = _code(dY, "dY"), _token_bits(tokens)
+    code = _code(dY, "dY")
+    bits = _TOKEN_BITS.get(tokens.dtype) or _refuse(f"tokens are int32 or int64, not {tokens.dtype}")
     if dY.dim() == 0 or dY.shape[:-1] != tokens.shape or dY.shape[-1] == 0 or vocab <= 0:
         raise ValueError(f"dY {tuple(dY.shape)} for tokens {tuple(tokens.shape)} of a vocabulary of {vocab}")
     if accumulate and out is None:
         raise ValueError("accumulate: out is needed")
-    device, hidden = dY.device, dY.shape[-1]
-    _same_device(device, tokens=tokens, out=out, work=work)
-    with _on(device):
-        tokens = tokens.contiguous()
-        if not (dY.is_contiguous() or (dY.dim() == 2 and dY.stride(1) == 1 and dY.stride(0) >= hidden)):
-            dY = dY.contiguous()
-        if out is None:
-            out = torch.empty(vocab, hidden, dtype=dY.dtype, device=device)
-        elif out.shape != (vocab, hidden):
-            raise ValueError(f"out: {(vocab, hidden)} is needed, not {tuple(out.shape)}")
-        if work is None:
-            work = torch.empty(lib().fira_embedding_grad_work_bytes(tokens.numel(), vocab, hidden, code), dtype=torch.uint8,
-                               device=device)
-        check(lib().fira_embedding_grad(tokens.data_ptr(), bits, tokens.numel(), dY.data_ptr(), _pitch(dY, "dY"), code, vocab,
-                                        hidden, scale, out.data_ptr(), _pitch(out, "out"), _code(out, "out"),
-                                        1 if accumulate else 0, work.data_ptr(), work.numel() * work.element_size(),
-                                        torch.cuda.current_stream().cuda_stream))
+    hidden = dY.shape[-1]
+    index = _device_of(dY, tokens, out, work)
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return embedding_grad(tokens, dY, vocab, scale, out, accumulate, work)
+    L, count = lib(), tokens.numel()
+    tokens, dY = tokens.contiguous(), _rows_or_copy(dY)
+    if out is None:
+        out = dY.new_empty((vocab, hidden))
+    elif out.shape != (vocab, hidden):
+        raise ValueError(f"out: {(vocab, hidden)} is needed, not {tuple(out.shape)}")
+    if work is None:
+        work = torch.empty(L.fira_embedding_grad_work_bytes(count, vocab, hidden, code), dtype=torch.uint8, device=dY.device)
+    status = L.fira_embedding_grad(tokens.data_ptr(), bits, count, dY.data_ptr(), _pitch(dY, "dY"), code, vocab, hidden, scale,
+                                   out.data_ptr(), _pitch(out, "out"), _code(out, "out"), 1 if accumulate else 0,
+                                   work.data_ptr(), work.nbytes, _raw_stream(index))
+    if status:
+        check(status)
     return out
 
 
 def _check_params(hidden: int, gain: torch.Tensor, bias: Optional[torch.Tensor], what: str) -> int:
     code = _code(gain, what)
     for p in (gain, bias):
-        if p is not None and (p.shape != (hidden,) or not p.is_contiguous() or p.dtype != gain.dtype):
+        if p is not None and (p.dim() != 1 or p.numel() != hidden or not p.is_contiguous() or p.dtype != gain.dtype):
             raise ValueError(f"{what}: contiguous vectors of {hidden} elements of one type are needed, not {tuple(p.shape)} "
                              f"of {p.dtype}")
     return code
@@ -399,6 +411,20 @@ def _check_stats(rows: int, mean: Optional[torch.Tensor], rstd: torch.Tensor, rm
             raise ValueError(f"mean and rstd: {rows} contiguous float32 numbers are needed")
 
 
+def _like(x: torch.Tensor, out: Optional[torch.Tensor]):
+    """A tensor for a result like x, given or new, and its pitch."""
+    if out is None:
+        return (torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)), 0
+    if out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError(f"out: {tuple(x.shape)} of {x.dtype} is needed, not {tuple(out.shape)} of {out.dtype}")
+    return out, _pitch(out, "out")
+
+
+def _address(t: torch.Tensor):
+    """A tensor's address; of an empty one, which has none, one that is not NULL and that nothing is read from."""
+    return t.data_ptr() or 256
+
+
 def layer_norm(x: torch.Tensor, gain: torch.Tensor, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
                rms: bool = False, out: Optional[torch.Tensor] = None):
     """fira_layer_norm over the last dimension: (y, mean, rstd); rms: the form without mean and bias (mean is None).  mean
@@ -406,20 +432,21 @@ def layer_norm(x: torch.Tensor, gain: torch.Tensor, bias: Optional[torch.Tensor]
     code = _code(x, "x")
     if x.dim() == 0 or x.shape[-1] == 0:
         raise ValueError(f"x has no rows: {tuple(x.shape)}")
-    device, hidden = x.device, x.shape[-1]
+    shape, hidden = x.shape[:-1], x.shape[-1]
     params = _check_params(hidden, gain, bias, "gain and bias")
-    _same_device(device, gain=gain, bias=bias, out=out)
     ld = _pitch(x, "x")
-    with _on(device):
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=device)
-        elif out.shape != x.shape or out.dtype != x.dtype:
-            raise ValueError(f"out: {tuple(x.shape)} of {x.dtype} is needed, not {tuple(out.shape)} of {out.dtype}")
-        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=device)
-        mean = None if rms else torch.empty_like(rstd)
-        check(lib().fira_layer_norm(x.data_ptr(), ld, code, rstd.numel(), hidden, gain.data_ptr(),
-                                    None if bias is None else bias.data_ptr(), params, eps, out.data_ptr(), _pitch(out, "out"),
-                                    None if rms else _address(mean), _address(rstd), torch.cuda.current_stream().cuda_stream))
+    index = _device_of(x, gain, bias, out)
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return layer_norm(x, gain, bias, eps, rms, out)
+    out, ld_out = _like(x, out)
+    rstd = x.new_empty(shape, dtype=torch.float32)
+    mean = None if rms else torch.empty_like(rstd)
+    status = lib().fira_layer_norm(x.data_ptr(), ld, code, rstd.numel(), hidden, gain.data_ptr(),
+                                   None if bias is None else bias.data_ptr(), params, eps, out.data_ptr(), ld_out,
+                                   None if rms else _address(mean), _address(rstd), _raw_stream(index))
+    if status:
+        check(status)
     return out, mean, rstd
 
 
@@ -427,13 +454,13 @@ def layer_norm_grad(dY: torch.Tensor, x: torch.Tensor, gain: torch.Tensor, mean:
                     rms: bool = False, out: Optional[torch.Tensor] = None, dgain: Optional[torch.Tensor] = None,
                     dbias: Optional[torch.Tensor] = None, accumulate: bool = False, work: Optional[torch.Tensor] = None):
     """fira_layer_norm_grad: (dX, dgain, dbias) from the gradient of y and from what layer_norm returned; dbias is None in
-    the form without mean.  out (dX): may be dY or x itself.  dgain, dbias: float32 or bfloat16, by default new tensors of the gain's type;
-    accumulate: added to what is in them.  work: a byte tensor of at least lib().fira_layer_norm_grad_work_bytes() bytes; by
-    default torch's allocator lends one for the call."""
+    the form without mean.  out (dX): may be dY or x itself.  dgain, dbias: float32 or bfloat16, by default new tensors of
+    the gain's type; accumulate: added to what is in them.  work: a byte tensor of at least
+    lib().fira_layer_norm_grad_work_bytes() bytes; by default torch's allocator lends one for the call."""
     code = _code(x, "x")
     if x.dim() == 0 or x.shape[-1] == 0 or dY.shape != x.shape or dY.dtype != x.dtype:
         raise ValueError(f"dY {tuple(dY.shape)} of {dY.dtype} for x {tuple(x.shape)} of {x.dtype}")
-    device, hidden = x.device, x.shape[-1]
+    hidden = x.shape[-1]
     rows = x.numel() // hidden
     params = _check_params(hidden, gain, None, "gain")
     _check_stats(rows, mean, rstd, rms)
@@ -441,27 +468,27 @@ def layer_norm_grad(dY: torch.Tensor, x: torch.Tensor, gain: torch.Tensor, mean:
         raise ValueError("the form without mean has no bias")
     if accumulate and (dgain is None or (dbias is None and not rms)):
         raise ValueError("accumulate: dgain and dbias are needed")
-    _same_device(device, dY=dY, gain=gain, mean=mean, rstd=rstd, out=out, dgain=dgain, dbias=dbias, work=work)
     ld = _pitch(x, "x")
-    with _on(device):
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=device)
-        elif out.shape != x.shape or out.dtype != x.dtype:
-            raise ValueError(f"out: {tuple(x.shape)} of {x.dtype} is needed, not {tuple(out.shape)} of {out.dtype}")
-        if not (dY.is_contiguous() or (dY.dim() == 2 and dY.stride(1) == 1 and dY.stride(0) >= hidden)):
-            dY = dY.contiguous()
-        if dgain is None:
-            dgain = torch.empty_like(gain)
-        if dbias is None and not rms:
-            dbias = torch.empty_like(dgain)
-        grads = _check_params(hidden, dgain, dbias, "dgain and dbias")
-        if work is None:
-            work = torch.empty(lib().fira_layer_norm_grad_work_bytes(rows, hidden, code) or 1, dtype=torch.uint8, device=device)
-        check(lib().fira_layer_norm_grad(dY.data_ptr(), _pitch(dY, "dY"), x.data_ptr(), ld, code, rows, hidden, gain.data_ptr(),
-                                         params, None if rms else _address(mean), rstd.data_ptr(), out.data_ptr(),
-                                         _pitch(out, "out"), dgain.data_ptr(), None if rms else dbias.data_ptr(), grads,
-                                         1 if accumulate else 0, work.data_ptr(), work.numel() * work.element_size(),
-                                         torch.cuda.current_stream().cuda_stream))
+    index = _device_of(x, dY, gain, mean, rstd, out, dgain, dbias, work)
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return layer_norm_grad(dY, x, gain, mean, rstd, rms, out, dgain, dbias, accumulate, work)
+    L = lib()
+    # a result over dY keeps its place, whatever becomes of dY's rows
+    (out, ld_out), dY = _like(x, out), _rows_or_copy(dY)
+    if dgain is None:
+        dgain = torch.empty_like(gain)
+    if dbias is None and not rms:
+        dbias = torch.empty_like(dgain)
+    grads = _check_params(hidden, dgain, dbias, "dgain and dbias")
+    if work is None:
+        work = torch.empty(L.fira_layer_norm_grad_work_bytes(rows, hidden, code) or 1, dtype=torch.uint8, device=x.device)
+    status = L.fira_layer_norm_grad(dY.data_ptr(), _pitch(dY, "dY"), x.data_ptr(), ld, code, rows, hidden, gain.data_ptr(),
+                                    params, None if rms else _address(mean), rstd.data_ptr(), out.data_ptr(), ld_out,
+                                    dgain.data_ptr(), None if rms else dbias.data_ptr(), grads, 1 if accumulate else 0,
+                                    work.data_ptr(), work.nbytes, _raw_stream(index))
+    if status:
+        check(status)
     return out, dgain, dbias
 
 
