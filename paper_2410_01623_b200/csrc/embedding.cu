@@ -132,6 +132,41 @@ __device__ __forceinline__ void place_entries(bool in, unsigned r, int position,
   __syncwarp();
 }
 
+// From the counts [warp][row] of a block's rows to the places of their positions: `front` is that of the first one.  Leaves
+// in counts where each warp's part of a row begins, and the rows' spans; returns the place behind the last one.
+__device__ __forceinline__ unsigned row_fronts(unsigned* counts, int warps, int nrows, unsigned front, int shift, unsigned me, int vocab, int2* span,
+                                               unsigned* sum_s) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int base = 0; base < nrows; base += blockDim.x) {
+    const int r = base + threadIdx.x;
+    unsigned count = 0;
+    if (r < nrows) {
+#pragma unroll 8
+      for (int w = 0; w < warps; ++w) {
+        const unsigned c = counts[w * nrows + r];
+        counts[w * nrows + r] = count;
+        count += c;
+      }
+    }
+    const unsigned inclusive = warp_inclusive(count);
+    if (lane == 31) sum_s[warp] = inclusive;
+    __syncthreads();
+    unsigned at = front + inclusive - count;
+    for (int w = 0; w < warps; ++w) {
+      if (w < warp) at += sum_s[w];
+      front += sum_s[w];
+    }
+    if (r < nrows) {
+      const long long v = ((long long)r << shift) + me;
+      if (v < vocab) span[v] = make_int2((int)at, (int)(at + count));
+#pragma unroll 8
+      for (int w = 0; w < warps; ++w) counts[w * nrows + r] += at;
+    }
+    __syncthreads();
+  }
+  return front;
+}
+
 // order: (position, token), equal tokens together; span[v]: where those of v begin and end; *total: tokens of the table.
 // Among equal tokens the order goes by warp (a stretch of positions each), step, place in the lane's four, lane.
 // Block b has the tokens v with v & (gridDim - 1) = b, in rows v >> shift.
@@ -180,36 +215,10 @@ k_token_order(const TOK* __restrict__ tokens, int n, int vocab, int shift, int n
   below = __reduce_add_sync(0xffffffffu, below);
   if (lane == 0) below_s[warp] = below;
   __syncthreads();
-  unsigned front = 0;                       // positions in front of the rows that are summed next
+  unsigned front = 0;
   for (int w = 0; w < warps; ++w) front += below_s[w];
-  for (int base = 0; base < nrows; base += threads) {
-    const int r = base + threadIdx.x;
-    unsigned count = 0;
-    if (r < nrows) {
-#pragma unroll 8
-      for (int w = 0; w < warps; ++w) {
-        const unsigned c = shared[w * nrows + r];
-        shared[w * nrows + r] = count;
-        count += c;
-      }
-    }
-    const unsigned inclusive = warp_inclusive(count);
-    if (lane == 31) sum_s[warp] = inclusive;
-    __syncthreads();
-    unsigned at = front + inclusive - count;
-    for (int w = 0; w < warps; ++w) {
-      if (w < warp) at += sum_s[w];
-      front += sum_s[w];
-    }
-    if (r < nrows) {
-      const long long v = ((long long)r << shift) + me;
-      if (v < vocab) span[v] = make_int2((int)at, (int)(at + count));
-#pragma unroll 8
-      for (int w = 0; w < warps; ++w) shared[w * nrows + r] += at;
-    }
-    __syncthreads();
-  }
-  if (me == mask && threadIdx.x == 0) *total = (int)front;
+  const unsigned end = row_fronts(shared, warps, nrows, front, shift, me, vocab, span, sum_s);
+  if (me == mask && threadIdx.x == 0) *total = (int)end;
   if (listed <= ORD_LIST) {
     for (int k = 0; k < listed; k += 32) {
       const bool in = k + lane < listed;
@@ -230,17 +239,109 @@ k_token_order(const TOK* __restrict__ tokens, int n, int vocab, int shift, int n
   }
 }
 
+// The same for large batches, in two launches: every block of k_token_order reads all tokens, which takes 36 us at 131072 of them
+// (and 8 at 4096); these read each token once.  k_token_split deals a tile of positions to the remainders, in their order;
+// entries [tile][ORD_TILE], and per remainder and tile how many there are (counts) and where they begin in the tile (fronts).
+constexpr int ORD_TILE = 1024;
+constexpr int ORD_SPLIT_FROM = 16384;       // positions from which on there are two launches (16384, hidden 512, fp32: 31 us both ways; 65536: 60 and 56)
+constexpr int ORD_SPLIT_BLOCKS = 512;       // remainders that k_token_split has counts for
+
+template <typename TOK>
+__global__ void __launch_bounds__(ORD_TILE)
+k_token_split(const TOK* __restrict__ tokens, int n, int vocab, int blocks, int2* __restrict__ entries, int* __restrict__ counts, int* __restrict__ fronts,
+              unsigned* __restrict__ counters, long long ncounters) {
+  extern __shared__ unsigned shared[];      // [32 warps][blocks]
+  __shared__ unsigned sum_s[32];
+  ptx::grid_launch_next();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tile = blockIdx.x, tiles = gridDim.x;
+  for (long long i = (long long)tile * ORD_TILE + threadIdx.x; i < ncounters; i += (long long)tiles * ORD_TILE) counters[i] = 0;
+  for (int i = threadIdx.x; i < 32 * blocks; i += ORD_TILE) shared[i] = 0;
+  const int position = tile * ORD_TILE + threadIdx.x;
+  const int token = position < n ? token_at(tokens, position, vocab) : -1;
+  const unsigned home = (unsigned)token & (unsigned)(blocks - 1);
+  __syncthreads();
+  const unsigned same = __match_any_sync(0xffffffffu, token >= 0 ? home : 0x80000000u | lane);
+  if (token >= 0 && lane == __ffs(same) - 1) shared[warp * blocks + home] = __popc(same);
+  __syncthreads();
+  const int h = threadIdx.x;
+  unsigned count = 0;
+  if (h < blocks) {
+#pragma unroll 8
+    for (int w = 0; w < 32; ++w) {
+      const unsigned c = shared[w * blocks + h];
+      shared[w * blocks + h] = count;
+      count += c;
+    }
+  }
+  const unsigned inclusive = warp_inclusive(count);
+  if (lane == 31) sum_s[warp] = inclusive;
+  __syncthreads();
+  if (h < blocks) {
+    unsigned at = inclusive - count;
+    for (int w = 0; w < warp; ++w) at += sum_s[w];
+    counts[(long long)h * tiles + tile] = (int)count;
+    fronts[(long long)h * tiles + tile] = (int)at;
+#pragma unroll 8
+    for (int w = 0; w < 32; ++w) shared[w * blocks + h] += at;
+  }
+  __syncthreads();
+  if (token >= 0) entries[(long long)tile * ORD_TILE + shared[warp * blocks + home] + __popc(same & ((1u << lane) - 1))] = make_int2(position, token);
+}
+
+// Block b sorts the entries of remainder b by row; a warp takes the tiles of a stretch.  Otherwise as k_token_order.
+__global__ void __launch_bounds__(ORD_MAX_THREADS)
+k_token_gather(const int2* entries, const int* counts, const int* fronts, int tiles, int vocab, int shift, int nrows, int2* order, int2* span, int* total) {
+  extern __shared__ unsigned shared[];      // counts [warps][nrows]
+  __shared__ unsigned below_s[32], sum_s[32];
+  ptx::grid_launch_next();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, threads = blockDim.x;
+  const unsigned me = blockIdx.x;
+  for (int i = threadIdx.x; i < warps * nrows; i += threads) shared[i] = 0;
+  ptx::grid_wait();
+  counts += (long long)me * tiles;
+  fronts += (long long)me * tiles;
+  unsigned below = 0;
+  for (int t = threadIdx.x; t < tiles; t += threads) below += fronts[t];
+  below = __reduce_add_sync(0xffffffffu, below);
+  if (lane == 0) below_s[warp] = below;
+  __syncthreads();
+  unsigned* mine = shared + warp * nrows;
+  const int per_warp = (tiles + warps - 1) / warps, t0 = min(tiles, warp * per_warp), t1 = min(tiles, t0 + per_warp);
+  for (int t = t0; t < t1; ++t) {
+    const int c = counts[t];
+    const int2* e = entries + (long long)t * ORD_TILE + fronts[t];
+    for (int k = lane; k < c; k += 32) atomicAdd(&mine[(unsigned)e[k].y >> shift], 1u);
+  }
+  __syncthreads();
+  unsigned front = 0;
+  for (int w = 0; w < warps; ++w) front += below_s[w];
+  const unsigned end = row_fronts(shared, warps, nrows, front, shift, me, vocab, span, sum_s);
+  if (me == gridDim.x - 1 && threadIdx.x == 0) *total = (int)end;
+  for (int t = t0; t < t1; ++t) {
+    const int c = counts[t];
+    const int2* e = entries + (long long)t * ORD_TILE + fronts[t];
+    for (int k = 0; k < c; k += 32) {
+      const bool in = k + lane < c;
+      const int2 x = in ? e[k + lane] : make_int2(0, 0);
+      place_entries(in, (unsigned)x.y >> shift, x.x, x.y, mine, order);
+    }
+  }
+}
+
 // ------------------------------------------------------------------------------------------------ sums of the rows
 constexpr int TG_DEPTH = 4;                 // rows of dY of a warp on their way
-constexpr int TG_MIN = 16;                  // positions of a stretch at least
+constexpr int TG_MIN = 8;                   // positions of a stretch at least
+constexpr int TG_GROUP = 16;                // stretches whose parts of a long row are added by one warp
 constexpr int TG_ZERO_ROWS = 64;            // rows that a block looks over for tokens
-constexpr int TG_ZERO_EARLY = 16384;        // tokens up to which such a block looks through them itself
+constexpr int TG_ZERO_EARLY = 16384;        // tokens up to which such a block looks through them itself (1024: 20.8 us, or 21.9; 16384: 31.0 and 32.1)
 
 struct TablePlan {
-  int shift, blocks, nrows, threads;        // k_token_order
+  int shift, blocks, nrows, threads;        // of the order of the tokens
+  int tiles;                                // k_token_split; 0: k_token_order
   long long chunks;                         // stretches of the order
   int slices, pieces;
-  size_t off_span, off_total, off_counters, off_parts, bytes;
+  long long counters() const { return 3 * chunks * slices; }     // per place of a part, and per stretch in which a long row begins
+  size_t off_span, off_total, off_counters, off_entries, off_counts, off_fronts, off_parts, bytes;
 };
 
 // The columns of a warp: PIECES times 32 lanes of 16 bytes of dY.
@@ -404,21 +505,39 @@ k_table_grad(const int2* order, const int2* span, const int* total, unsigned* co
     } else {
       const int s = v == v_first ? first_s : last_s, e = v == v_first ? first_e : last_e;
       const long long c0 = s / T, c1 = (e - 1) / T;
-      // two long rows may meet in a chunk: the one that begins there has the second place
-      auto part = [&](long long c) { return parts + ((2 * c + (c == c0 ? 1 : 0)) * slices + slice) * Cols::WIDTH; };
-      at.store_part(part(chunk), sum);
-      __threadfence();
-      __syncwarp();
-      unsigned before = 0;
-      if (lane == 0) before = atomicAdd(&counters[c0 * slices + slice], 1u);
-      before = __shfl_sync(0xffffffffu, before, 0);
-      if (before == (unsigned)(c1 - c0)) {  // all parts are there
+      // two long rows may meet in a stretch: the one that begins there has the second place
+      auto place = [&](long long c) { return (2 * c + (c == c0 ? 1 : 0)) * slices + slice; };
+      // Whether this warp is the last of n at a counter; what the others stored is then there.
+      auto last_of = [&](unsigned* counter, long long n) {
         __threadfence();
+        __syncwarp();
+        unsigned before = 0;
+        if (lane == 0) before = atomicAdd(counter, 1u);
+        before = __shfl_sync(0xffffffffu, before, 0);
+        __threadfence();
+        return before == (unsigned)(n - 1);
+      };
+      auto add_parts = [&](long long from, long long to, long long step) {
 #pragma unroll
         for (int k = 0; k < N; ++k) sum[k] = 0.f;
+        const long long first = from / step * step;         // (in steps that are counted from 0, but not below `from`)
 #pragma unroll 4
-        for (long long c = c0; c <= c1; ++c) at.add_part(part(c), sum);
-        at.store(G + v * ldg, sum, scale, add);
+        for (long long c = first; c <= to; c += step) at.add_part(parts + place(max(c, from)) * Cols::WIDTH, sum);
+      };
+      // The parts of a group of stretches are added by the last of its warps, and left in the place of the first; the groups'
+      // sums by the last group's.
+      const long long group = chunk / TG_GROUP, from = max(c0, group * TG_GROUP), to = min(c1, group * TG_GROUP + TG_GROUP - 1);
+      const long long ngroups = c1 / TG_GROUP - c0 / TG_GROUP + 1;
+      at.store_part(parts + place(chunk) * Cols::WIDTH, sum);
+      if (last_of(&counters[place(from)], to - from + 1)) {
+        add_parts(from, to, 1);
+        bool last = ngroups == 1;
+        if (!last) {
+          at.store_part(parts + place(from) * Cols::WIDTH, sum);
+          last = last_of(&counters[(2 * chunks + c0) * slices + slice], ngroups);
+          if (last) add_parts(c0, c1, TG_GROUP);
+        }
+        if (last) at.store(G + v * ldg, sum, scale, add);
       }
     }
 #pragma unroll
@@ -479,6 +598,7 @@ TablePlan plan_for(long long n, long long vocab, long long hidden, bool f32) {
   p.shift = 0;
   while ((1 << p.shift) < p.blocks) ++p.shift;
   p.nrows = (int)((vocab + p.blocks - 1) / p.blocks);
+  p.tiles = n > ORD_SPLIT_FROM && p.blocks <= ORD_SPLIT_BLOCKS ? (int)((n + ORD_TILE - 1) / ORD_TILE) : 0;
   // every warp has counts of its own, which cost time per warp: few warps for few tokens
   p.threads = n > 32768 ? ORD_MAX_THREADS : n > 8192 ? 512 : 256;
   // 512 bytes of dY per warp and row, or 1024, which takes fewer instructions per byte
@@ -492,7 +612,10 @@ TablePlan plan_for(long long n, long long vocab, long long hidden, bool f32) {
   size_t at = align_up((size_t)n * sizeof(int2));
   p.off_span = at; at += align_up((size_t)vocab * sizeof(int2));
   p.off_total = at; at += 256;
-  p.off_counters = at; at += align_up((size_t)p.chunks * p.slices * sizeof(unsigned));
+  p.off_counters = at; at += align_up((size_t)p.counters() * sizeof(unsigned));
+  p.off_entries = at; at += (size_t)p.tiles * ORD_TILE * sizeof(int2);
+  p.off_counts = at; at += align_up((size_t)p.tiles * p.blocks * sizeof(int));
+  p.off_fronts = at; at += align_up((size_t)p.tiles * p.blocks * sizeof(int));
   p.off_parts = at; at += (size_t)p.chunks * 2 * p.slices * width * sizeof(float);
   p.bytes = align_up(std::max<size_t>(at, 256));
   return p;
@@ -521,8 +644,30 @@ void run_lookup(const void* table, long long ld, const void* tokens, long long n
 }
 
 // Counts and lists may be above the default limit of shared memory: a setting per device and kernel.
+template <typename TOK>
+cudaError_t run_split(const TablePlan& p, const void* tokens, int n, int vocab, char* work, cudaStream_t st) {
+  const size_t smem = (size_t)32 * p.blocks * sizeof(unsigned), gather = (size_t)(p.threads / 32) * p.nrows * sizeof(unsigned);
+  if (smem > 47 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(k_token_split<TOK>, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * ORD_SPLIT_BLOCKS * 4);
+    if (e != cudaSuccess) return e;
+  }
+  if (gather > 47 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(k_token_gather, cudaFuncAttributeMaxDynamicSharedMemorySize, ORD_MAX_THREADS / 32 * ORD_MAX_ROWS * 4);
+    if (e != cudaSuccess) return e;
+  }
+  int2* entries = (int2*)(work + p.off_entries);
+  int* counts = (int*)(work + p.off_counts);
+  int* fronts = (int*)(work + p.off_fronts);
+  k_token_split<TOK><<<p.tiles, ORD_TILE, smem, st>>>((const TOK*)tokens, n, vocab, p.blocks, entries, counts, fronts, (unsigned*)(work + p.off_counters),
+                                                      p.counters());
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  return launch_chained(k_token_gather, dim3(p.blocks), p.threads, gather, st, true, 1, (const int2*)entries, (const int*)counts, (const int*)fronts, p.tiles,
+                        vocab, p.shift, p.nrows, (int2*)work, (int2*)(work + p.off_span), (int*)(work + p.off_total));
+}
 template <typename TOK, bool VECTOR>
 cudaError_t run_order(const TablePlan& p, const void* tokens, int n, int vocab, char* work, cudaStream_t st) {
+  if (p.tiles) return run_split<TOK>(p, tokens, n, vocab, work, st);
   auto bytes = [](int warps, int nrows) { return (size_t)((warps * nrows + 1) & ~1) * sizeof(unsigned) + (size_t)warps * ORD_LIST * sizeof(int2); };
   const size_t smem = bytes(p.threads / 32, p.nrows);
   if (smem > 47 * 1024) {
@@ -530,7 +675,7 @@ cudaError_t run_order(const TablePlan& p, const void* tokens, int n, int vocab, 
     if (e != cudaSuccess) return e;
   }
   k_token_order<TOK, VECTOR><<<p.blocks, p.threads, smem, st>>>((const TOK*)tokens, n, vocab, p.shift, p.nrows, (int2*)work, (int2*)(work + p.off_span),
-                                                                (int*)(work + p.off_total), (unsigned*)(work + p.off_counters), p.chunks * p.slices);
+                                                                (int*)(work + p.off_total), (unsigned*)(work + p.off_counters), p.counters());
   return cudaGetLastError();
 }
 

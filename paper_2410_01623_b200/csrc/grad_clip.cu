@@ -25,9 +25,11 @@ constexpr int GC_CHUNK = 8;                       // elements of a chunk: 16 byt
 constexpr int GC_UNROLL = 4;                      // chunks of a thread in flight
 constexpr int GC_TILE = GC_THREADS * GC_UNROLL;   // chunks of a tile (8192 elements)
 constexpr int GC_SMS = 148;
-constexpr int GC_BLOCKS = GC_SMS * 4;             // blocks of a launch: tiles are dealt to them in turn
+constexpr int GC_BLOCKS = GC_SMS * 4;             // blocks of the sums, all resident: tiles are dealt to them in turn
+constexpr int GC_SCALE_BLOCKS = GC_SMS * 32;      // of the scaling: eight times as many as are resident, since SMs far from the
+                                                  // memory take longer (2.7 GB of bf16: 925 us with 4 per SM, 831 so, as long as a copy)
 constexpr int GC_MANY = 480, GC_FEW = 48;         // tensors of a launch: 31 KB of kernel arguments, or 3.1 KB
-constexpr long long GC_KEPT = 80ll << 20;         // bytes that the scaling finds in L2 (126 MB, which its stores share)
+constexpr long long GC_KEPT = 48ll << 20;         // bytes that the sums leave in L2 for the scaling (232 MB of fp32: 110 -> 104 us)
 
 // One tensor.  A flat one is one row; rows of a pitched one start on their own.
 struct GradEntry {
@@ -124,11 +126,11 @@ __device__ __forceinline__ void store_chunk(const GradEntry& t, const Place& p, 
   }
 }
 
-// L2 policies.  What is read once or written for somebody later makes room for what the scaling reads again.
+// L2 policies.  What is read once makes room for what the scaling reads again, after which that is to go first too.
 __device__ __forceinline__ uint64_t policy(bool first) {
   uint64_t p;
   if (first) asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
-  else asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
+  else asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
   return p;
 }
 __device__ __forceinline__ uint4 load16(const void* p, uint64_t pol) {
@@ -227,9 +229,9 @@ __device__ __forceinline__ double whole_squares(const void* g, long long first, 
   return squares(v);
 }
 template <int W, bool OUT_BF16>
-__device__ __forceinline__ void whole_scale(const void* g, void* o, long long first, float scale, uint64_t load_pol, uint64_t store_pol) {
+__device__ __forceinline__ void whole_scale(const void* g, void* o, long long first, float scale, uint64_t pol) {
   uint4 u[W];
-  load_whole<W>(g, first, load_pol, u);
+  load_whole<W>(g, first, pol, u);
 #pragma unroll
   for (int i = 0; i < W; ++i) {
     constexpr int N = GC_ELEMS / W;
@@ -241,13 +243,13 @@ __device__ __forceinline__ void whole_scale(const void* g, void* o, long long fi
     const long long at = (first * (W / GC_UNROLL) + i * GC_THREADS + threadIdx.x) * N;
     if constexpr (OUT_BF16) {
       __nv_bfloat16* q = static_cast<__nv_bfloat16*>(o) + at;
-      if constexpr (N == 8) store16(q, make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])), store_pol);
-      else store8(q, pack2(v[0], v[1]), pack2(v[2], v[3]), store_pol);
+      if constexpr (N == 8) store16(q, make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])), pol);
+      else store8(q, pack2(v[0], v[1]), pack2(v[2], v[3]), pol);
     } else {
       float* q = static_cast<float*>(o) + at;
 #pragma unroll
       for (int e = 0; e < N; e += 4)
-        store16(q + e, make_uint4(__float_as_uint(v[e]), __float_as_uint(v[e + 1]), __float_as_uint(v[e + 2]), __float_as_uint(v[e + 3])), store_pol);
+        store16(q + e, make_uint4(__float_as_uint(v[e]), __float_as_uint(v[e + 1]), __float_as_uint(v[e + 2]), __float_as_uint(v[e + 3])), pol);
     }
   }
 }
@@ -307,7 +309,7 @@ k_grad_norm(const double* sums, int nsums, float* norm_out) {
 template <int CAP>
 __global__ void __launch_bounds__(GC_THREADS, 4)
 k_grad_scale(const __grid_constant__ GradTable<CAP> tab, const double* sums, int nsums, float max_norm, float* norm_out, float* scale_out,
-             int in_place, int kept) {
+             int in_place) {
   __shared__ double red[GC_THREADS / 32];
   ptx::grid_wait();
   const double norm = norm_of(sums, nsums, red);
@@ -315,7 +317,7 @@ k_grad_scale(const __grid_constant__ GradTable<CAP> tab, const double* sums, int
   const float scale = finite && norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.f;
   if (blockIdx.x == 0 && threadIdx.x == 0) { *norm_out = (float)norm; *scale_out = scale; }
   if (in_place && scale == 1.f) return;
-  const uint64_t once = policy(true), later = policy(false);
+  const uint64_t once = policy(true);
   int q = tab.count - 1;
   // from the end: what the sums read last is what the L2 still holds
   for (int tile = tab.tiles - 1 - (int)blockIdx.x; tile >= 0; tile -= gridDim.x) {
@@ -323,13 +325,12 @@ k_grad_scale(const __grid_constant__ GradTable<CAP> tab, const double* sums, int
     const GradEntry& t = tab.t[q];
     if (tile - t.tile_start < t.whole) {
       const long long first = (long long)(tile - t.tile_start) * GC_TILE;
-      const uint64_t pol = tile >= kept ? once : later;       // (no store takes the place of what is still to be read)
       if (t.bf16) {
-        if (t.out_bf16) whole_scale<4, true>(t.g, t.o, first, scale, once, pol);
-        else whole_scale<4, false>(t.g, t.o, first, scale, once, pol);
+        if (t.out_bf16) whole_scale<4, true>(t.g, t.o, first, scale, once);
+        else whole_scale<4, false>(t.g, t.o, first, scale, once);
       } else {
-        if (t.out_bf16) whole_scale<8, true>(t.g, t.o, first, scale, once, pol);
-        else whole_scale<8, false>(t.g, t.o, first, scale, once, pol);
+        if (t.out_bf16) whole_scale<8, true>(t.g, t.o, first, scale, once);
+        else whole_scale<8, false>(t.g, t.o, first, scale, once);
       }
     } else {
       Place p[GC_UNROLL];
@@ -458,9 +459,9 @@ cudaError_t run_list(int32_t count, const fira_grad_desc* descs, const void* con
   bool chained = true;          // only behind the sums: a second part of a long list runs behind a kernel that lets it in at its end
   for (int base = (count - 1) / CAP * CAP; base >= 0; base -= CAP) {
     if (count > CAP) fill(tab, base, std::min(CAP, count - base), descs, G_dev, out_dev);
-    const int blocks = std::max(1, std::min(GC_BLOCKS, tab.tiles));
+    const int blocks = std::max(1, std::min(GC_SCALE_BLOCKS, tab.tiles));
     const cudaError_t e = launch_chained(k_grad_scale<CAP>, dim3(blocks), GC_THREADS, 0, st, chained, 1, tab, (const double*)sums, nsums,
-                                         max_norm, norm_dev, scale_dev, out_dev == nullptr ? 1 : 0, kept_from(tab));
+                                         max_norm, norm_dev, scale_dev, out_dev == nullptr ? 1 : 0);
     if (e != cudaSuccess) return e;
     chained = false;
   }
