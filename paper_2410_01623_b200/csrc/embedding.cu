@@ -332,7 +332,8 @@ k_token_gather(const int2* entries, const int* counts, const int* fronts, int ti
 constexpr int TG_DEPTH = 4;                 // rows of dY of a warp on their way
 constexpr int TG_MIN = 8;                   // positions of a stretch at least
 constexpr int TG_GROUP = 16;                // stretches whose parts of a long row are added by one warp
-constexpr int TG_ZERO_ROWS = 64;            // rows that a block looks over for tokens
+constexpr int TG_ZERO_ROWS = 64;            // rows that a block looks over for tokens, or TG_ZERO_MOST, where looking costs more
+constexpr int TG_ZERO_MOST = 256;           // (16384 tokens, hidden 512, fp32: 31.8 us with 64 rows, 29.6 with 256; 32768 tokens: 41 and 51)
 constexpr int TG_ZERO_EARLY = 16384;        // tokens up to which such a block looks through them itself (1024: 20.8 us, or 21.9; 16384: 31.0 and 32.1)
 
 struct TablePlan {
@@ -424,14 +425,16 @@ struct Slice {
   }
 };
 
+__host__ __device__ constexpr int zero_rows_of(int ntokens) { return ntokens > 4096 && ntokens <= TG_ZERO_EARLY ? TG_ZERO_MOST : TG_ZERO_ROWS; }
+
 // Zeroes the rows of `first` on that no token names.  early: in front of the wait for k_token_order, from the tokens.
 template <typename TO, typename TOK, bool VECTOR>
-__device__ __forceinline__ void zero_rows(long long first, int vocab, int hidden, const int2* span, const TOK* __restrict__ tokens, int n, bool early, TO* G,
+__device__ __forceinline__ void zero_rows(long long first, int zero_rows_each, int vocab, int hidden, const int2* span, const TOK* __restrict__ tokens, int n, bool early, TO* G,
                                           long long ldg) {
-  __shared__ unsigned char named[TG_ZERO_ROWS];
-  const int here = (int)min((long long)TG_ZERO_ROWS, vocab - first);
+  __shared__ unsigned char named[TG_ZERO_MOST];
+  const int here = (int)min((long long)zero_rows_each, vocab - first);
   if (early) {
-    for (int k = threadIdx.x; k < TG_ZERO_ROWS; k += EM_THREADS) named[k] = 0;
+    for (int k = threadIdx.x; k < TG_ZERO_MOST; k += EM_THREADS) named[k] = 0;
     __syncthreads();
 #pragma unroll 8
     for (int i = threadIdx.x; i < n; i += EM_THREADS) {
@@ -460,7 +463,7 @@ __device__ __forceinline__ void zero_rows(long long first, int vocab, int hidden
   }
 }
 
-// zero_blocks blocks zero, TG_ZERO_ROWS rows each; the warps of the others take a stretch of T positions and a slice each.
+// zero_blocks blocks zero, zero_rows_of() rows each; the warps of the others take a stretch of T positions and a slice each.
 template <typename TI, typename TO, typename TOK, bool VECTOR, int PIECES>
 __global__ void __launch_bounds__(EM_THREADS, PIECES == 1 ? 4 : 3)
 k_table_grad(const int2* order, const int2* span, const int* total, unsigned* counters, float* parts, const TOK* __restrict__ tokens, int ntokens,
@@ -473,7 +476,8 @@ k_table_grad(const int2* order, const int2* span, const int* total, unsigned* co
   const bool early = ntokens <= TG_ZERO_EARLY;
   const int main_blocks = gridDim.x - zero_blocks, block = early ? (int)blockIdx.x - zero_blocks : (int)blockIdx.x;
   if (block < 0 || block >= main_blocks) {
-    zero_rows<TO, TOK, VECTOR>((long long)(early ? blockIdx.x : block - main_blocks) * TG_ZERO_ROWS, vocab, hidden, span, tokens, ntokens, early, G, ldg);
+    const int each = zero_rows_of(ntokens);
+    zero_rows<TO, TOK, VECTOR>((long long)(early ? blockIdx.x : block - main_blocks) * each, each, vocab, hidden, span, tokens, ntokens, early, G, ldg);
     ptx::grid_wait();                       // (this kernel does not end before the one in front of it)
     return;
   }
@@ -605,9 +609,11 @@ TablePlan plan_for(long long n, long long vocab, long long hidden, bool f32) {
   p.pieces = hidden > 32 * (f32 ? 4 : 8) ? 2 : 1;
   const long long width = 32 * (f32 ? 4 : 8) * p.pieces;
   p.slices = (int)((hidden + width - 1) / width);
-  // As many stretches as there are warps on the GPU at once, all of one length, which follows from the number of tokens
-  // that the device finds; of few positions as many as have TG_MIN each.
-  p.chunks = std::max<long long>(1, std::min<long long>((n + TG_MIN - 1) / TG_MIN, EM_SMS * (p.pieces == 2 ? 3 : 4) * EM_WARPS / p.slices));
+  // As many stretches as there are warps on the GPU at once, or four times as many where that leaves 32 positions each (131072 tokens,
+  // hidden 2048, bf16: 142 us, 133 so; hidden 512: 60, and 69 with four times as many of 8); of few positions as many as
+  // have TG_MIN each.  All are of one length, which follows from the number of tokens that the device finds.
+  const long long warps = EM_SMS * (p.pieces == 2 ? 3 : 4) * EM_WARPS;
+  p.chunks = std::max<long long>(1, std::max(std::min((n + TG_MIN - 1) / TG_MIN, warps / p.slices), std::min(n / 32, 4 * warps / p.slices)));
   if (n == 0) p.chunks = 0;
   size_t at = align_up((size_t)n * sizeof(int2));
   p.off_span = at; at += align_up((size_t)vocab * sizeof(int2));
@@ -682,7 +688,7 @@ cudaError_t run_order(const TablePlan& p, const void* tokens, int n, int vocab, 
 template <typename TI, typename TO, typename TOK>
 cudaError_t run_grad(const TablePlan& p, const void* tokens, int n, const void* dY, long long ld, int vocab, int hidden, float scale, int add, void* G, long long ldg, char* work,
                      bool vector, cudaStream_t st) {
-  const int zero_blocks = add ? 0 : (vocab + TG_ZERO_ROWS - 1) / TG_ZERO_ROWS;
+  const int zero_blocks = add ? 0 : (vocab + zero_rows_of(n) - 1) / zero_rows_of(n);
   const dim3 grid((unsigned)(zero_blocks + (p.chunks * p.slices + EM_WARPS - 1) / EM_WARPS));
   if (grid.x == 0) return cudaSuccess;
   auto kernel = p.pieces == 2 ? (vector ? k_table_grad<TI, TO, TOK, true, 2> : k_table_grad<TI, TO, TOK, false, 2>)
