@@ -35,8 +35,10 @@ __device__ __forceinline__ int token_at(const TOK* tokens, long long i, int voca
   return t >= 0 && t < vocab ? (int)t : -1;
 }
 
-// A warp takes LK_ROWS positions and a slice of the columns.
-template <typename T, typename TOK, bool VECTOR>
+// A warp takes LK_ROWS positions and a slice of the columns.  ALIGNED: all rows are whole 16-byte units on 16-byte boundaries.
+// Otherwise a lane has 16 aligned bytes of the output row and funnels them from two aligned words of the table, of which it
+// reads those that hold a byte of them.
+template <typename T, typename TOK, bool ALIGNED>
 __global__ void __launch_bounds__(EM_THREADS)
 k_embedding(const T* __restrict__ table, long long ld, const TOK* __restrict__ tokens, long long n, int vocab, int hidden, int slices,
             float scale, T* __restrict__ out, long long ld_out) {
@@ -44,37 +46,43 @@ k_embedding(const T* __restrict__ table, long long ld, const TOK* __restrict__ t
   const int lane = threadIdx.x & 31;
   const long long unit = (long long)blockIdx.x * EM_WARPS + (threadIdx.x >> 5);
   const long long i0 = unit / slices * LK_ROWS;
-  const int col0 = (int)(unit % slices) * 32 * N;
+  const int col0 = ((int)(unit % slices) * 32 + lane) * N;
   if (i0 >= n) return;
   int t[LK_ROWS];
 #pragma unroll
   for (int u = 0; u < LK_ROWS; ++u) t[u] = i0 + u < n ? token_at(tokens, i0 + u, vocab) : -1;
-  if (VECTOR) {
-    const int col = col0 + lane * N;
-    if (col >= hidden) return;
-    float v[LK_ROWS][N];
+  uint4 a[LK_ROWS], b[LK_ROWS];
 #pragma unroll
-    for (int u = 0; u < LK_ROWS; ++u) {
-#pragma unroll
-      for (int e = 0; e < N; ++e) v[u][e] = 0.f;
-      if (t[u] >= 0) rows::load_vec<T, N>(table + (long long)t[u] * ld + col, v[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < LK_ROWS; ++u) {
-      if (i0 + u >= n) break;
-#pragma unroll
-      for (int e = 0; e < N; ++e) v[u][e] *= scale;
-      rows::store_vec<T, N>(out + (i0 + u) * ld_out + col, v[u]);
-    }
-  } else {
-#pragma unroll
-    for (int u = 0; u < LK_ROWS; ++u) {
-      if (i0 + u >= n) break;
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const int col = col0 + e * 32 + lane;
-        if (col < hidden) out[(i0 + u) * ld_out + col] = from_float<T>(t[u] >= 0 ? scale * to_float<T>(table[(long long)t[u] * ld + col]) : 0.f);
+  for (int u = 0; u < LK_ROWS; ++u) {
+    a[u] = b[u] = make_uint4(0u, 0u, 0u, 0u);
+    const T* row = table + (long long)t[u] * ld;
+    if (ALIGNED) {
+      if (t[u] >= 0 && col0 < hidden) a[u] = *reinterpret_cast<const uint4*>(row + col0);
+    } else {
+      const int col = col0 - (int)(((uintptr_t)(out + (i0 + u) * ld_out) & 15) / sizeof(T));
+      const uintptr_t from = (uintptr_t)(row + max(col, 0)), end = (uintptr_t)(row + min(col + N, hidden));      // the bytes that are wanted
+      const uintptr_t word = (uintptr_t)(row + col) & ~(uintptr_t)15;
+      if (t[u] >= 0 && from < end) {
+        if (word + 16 > from) a[u] = *reinterpret_cast<const uint4*>(word);
+        if (word + 16 < end) b[u] = *reinterpret_cast<const uint4*>(word + 16);
       }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < LK_ROWS; ++u) {
+    if (i0 + u >= n) break;
+    T* row = out + (i0 + u) * ld_out;
+    const int col = ALIGNED ? col0 : col0 - (int)(((uintptr_t)row & 15) / sizeof(T));
+    if (!ALIGNED) a[u] = rows::funnel16(a[u], b[u], (int)((uintptr_t)(table + (long long)t[u] * ld + col) & 15));
+    float2 v[N / 2];
+    rows::unpack<T>(a[u], v);
+#pragma unroll
+    for (int e = 0; e < N / 2; ++e) v[e] = rows::mul2(v[e], rows::both(scale));
+    const uint4 w = rows::pack<T>(v);
+    if (ALIGNED) {
+      if (col < hidden) *reinterpret_cast<uint4*>(row + col) = w;
+    } else {
+      rows::store_between(row + col, w, col, 0, hidden);
     }
   }
 }
@@ -345,46 +353,54 @@ struct TablePlan {
   size_t off_span, off_total, off_counters, off_entries, off_counts, off_fronts, off_parts, bytes;
 };
 
-// The columns of a warp: PIECES times 32 lanes of 16 bytes of dY.
-template <typename TI, typename TO, bool VECTOR, int PIECES>
+// The columns of a warp: PIECES times 32 lanes of 16 bytes of dY.  ALIGNED: the rows of dY and G are whole 16-byte units on
+// 16-byte boundaries, and a lane reads the 16 bytes that it fetched itself.  Otherwise the warp fetches the aligned words that
+// hold a byte of its columns, one more than it has lanes, and a lane funnels its columns from two of them.
+template <typename TI, typename TO, bool ALIGNED, int PIECES>
 struct Slice {
-  static constexpr int E = rows::PER16<TI>, N = E * PIECES, WIDTH = 32 * N;
+  static constexpr int E = rows::PER16<TI>, N = E * PIECES, WIDTH = 32 * N, WORDS = 32 * PIECES + (ALIGNED ? 0 : 1);
   int col0, lane, hidden;
-  __device__ __forceinline__ int col(int p, int e) const { return col0 + p * 32 * E + (VECTOR ? lane * E + e : e * 32 + lane); }
-  // A row on its way to a slot, of which a lane reads its own.
-  __device__ __forceinline__ void fetch(const TI* row, uint4* slot) const {
+  __device__ __forceinline__ int col(int p) const { return col0 + (p * 32 + lane) * E; }
+  // A row on its way to a slot; *skip: where its columns begin in the slot.
+  __device__ __forceinline__ void fetch(const TI* row, uint4* slot, int* skip) const {
+    if (ALIGNED) {
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
-      if (VECTOR) {
-        if (col(p, 0) < hidden)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"((unsigned)__cvta_generic_to_shared(slot + p * 32 + lane)), "l"(row + col(p, 0)) : "memory");
-      } else {
-        TI* v = reinterpret_cast<TI*>(slot + p * 32 + lane);
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (col(p, e) < hidden) v[e] = row[col(p, e)];
-      }
+      for (int p = 0; p < PIECES; ++p)
+        if (col(p) < hidden)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"((unsigned)__cvta_generic_to_shared(slot + p * 32 + lane)), "l"(row + col(p)) : "memory");
+    } else {
+      const uintptr_t from = (uintptr_t)(row + col0), end = (uintptr_t)(row + min(col0 + WIDTH, hidden)), word = from & ~(uintptr_t)15;
+      for (int w = lane; w < WORDS; w += 32)
+        if (word + 16 * w < end)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"((unsigned)__cvta_generic_to_shared(slot + w)), "l"(word + 16 * w) : "memory");
+      if (lane == 0) *skip = (int)(from & 15);
     }
   }
-  __device__ __forceinline__ void add(const uint4* slot, float (&sum)[N]) const {
+  // Adds the row in a slot whose fetch has been waited for.  (Columns beyond the width: whatever is there, never stored.)
+  __device__ __forceinline__ void add(const uint4* slot, const int* skip, float (&sum)[N]) const {
+    if (!ALIGNED) __syncwarp();             // words that other lanes fetched
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       float2 v[E / 2];
-      rows::unpack<TI>(slot[p * 32 + lane], v);         // (columns beyond the width: whatever is there, never stored)
+      if (ALIGNED) rows::unpack<TI>(slot[p * 32 + lane], v);
+      else rows::unpack<TI>(rows::funnel16(slot[p * 32 + lane], slot[p * 32 + lane + 1], *skip), v);
 #pragma unroll
       for (int e = 0; e < E; e += 2) {
         const float2 s = rows::add2(make_float2(sum[p * E + e], sum[p * E + e + 1]), v[e / 2]);
         sum[p * E + e] = s.x; sum[p * E + e + 1] = s.y;
       }
     }
+    if (!ALIGNED) __syncwarp();             // the slot is filled anew
   }
+  // (All lanes of the warp.)
   __device__ __forceinline__ void store(TO* row, float (&sum)[N], float scale, bool add) const {
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       float* v = sum + p * E;
-      if (VECTOR) {
-        if (col(p, 0) >= hidden) continue;
-        TO* q = row + col(p, 0);
+      const int c = col(p);
+      if (ALIGNED) {
+        if (c >= hidden) continue;
+        TO* q = row + c;
         float w[E];
         if constexpr (E * sizeof(TO) % 16 == 0) {
           if (add) rows::load_vec<TO, E>(q, w);
@@ -402,12 +418,26 @@ struct Slice {
           const __nv_bfloat162 a = __floats2bfloat162_rn(w[0], w[1]), b = __floats2bfloat162_rn(w[2], w[3]);
           *reinterpret_cast<uint2*>(q) = make_uint2(*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b));
         }
+      } else if (sizeof(TO) == sizeof(TI) && !add) {
+        // the aligned word in which this lane's columns begin: its first bytes are the lane's before; the last lane has
+        // bytes left for one word more
+        if constexpr (sizeof(TO) == sizeof(TI)) {
+          float2 w[E / 2];
+#pragma unroll
+          for (int e = 0; e < E / 2; ++e) w[e] = rows::mul2(make_float2(v[2 * e], v[2 * e + 1]), rows::both(scale));
+          const uint4 own = rows::pack<TO>(w);
+          uint4 left;
+          left.x = __shfl_up_sync(0xffffffffu, own.x, 1); left.y = __shfl_up_sync(0xffffffffu, own.y, 1);
+          left.z = __shfl_up_sync(0xffffffffu, own.z, 1); left.w = __shfl_up_sync(0xffffffffu, own.w, 1);
+          const int behind = (int)((uintptr_t)(row + c) & 15), at = behind / (int)sizeof(TO);       // (the same in all lanes)
+          const int lo = col0 + p * 32 * E, hi = min(lo + 32 * E, hidden);
+          rows::store_between(row + c - at, behind ? rows::funnel16(left, own, 16 - behind) : own, c - at, lo, hi);
+          if (lane == 31 && behind) rows::store_between(row + c - at + E, rows::funnel16(own, own, 16 - behind), c - at + E, lo, hi);
+        }
       } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int c = col(p, e);
-          if (c < hidden) row[c] = from_float<TO>(add ? fmaf(scale, v[e], to_float<TO>(row[c])) : scale * v[e]);
-        }
+        for (int e = 0; e < E; ++e)
+          if (c + e < hidden) row[c + e] = from_float<TO>(add ? fmaf(scale, v[e], to_float<TO>(row[c + e])) : scale * v[e]);
       }
     }
   }
@@ -428,7 +458,7 @@ struct Slice {
 __host__ __device__ constexpr int zero_rows_of(int ntokens) { return ntokens > 4096 && ntokens <= TG_ZERO_EARLY ? TG_ZERO_MOST : TG_ZERO_ROWS; }
 
 // Zeroes the rows of `first` on that no token names.  early: in front of the wait for k_token_order, from the tokens.
-template <typename TO, typename TOK, bool VECTOR>
+template <typename TO, typename TOK, bool ALIGNED>
 __device__ __forceinline__ void zero_rows(long long first, int zero_rows_each, int vocab, int hidden, const int2* span, const TOK* __restrict__ tokens, int n, bool early, TO* G,
                                           long long ldg) {
   __shared__ unsigned char named[TG_ZERO_MOST];
@@ -453,31 +483,34 @@ __device__ __forceinline__ void zero_rows(long long first, int zero_rows_each, i
   for (int k = threadIdx.x >> 5; k < here; k += EM_WARPS) {
     if (named[k]) continue;
     TO* row = G + (first + k) * ldg;
-    if (VECTOR) {
+    if (ALIGNED) {
       const int bytes = hidden * (int)sizeof(TO);       // a multiple of 8
       for (int b = lane * 16; b + 16 <= bytes; b += 512) *reinterpret_cast<uint4*>(reinterpret_cast<char*>(row) + b) = make_uint4(0u, 0u, 0u, 0u);
       if (lane == 0 && (bytes & 8)) *reinterpret_cast<uint2*>(reinterpret_cast<char*>(row) + bytes - 8) = make_uint2(0u, 0u);
     } else {
-      for (int c = lane; c < hidden; c += 32) row[c] = from_float<TO>(0.f);
+      constexpr int N = rows::PER16<TO>;
+      const int at = (int)((uintptr_t)row & 15) / (int)sizeof(TO);
+      for (int c = lane * N - at; c < hidden; c += 32 * N) rows::store_between(row + c, make_uint4(0u, 0u, 0u, 0u), c, 0, hidden);
     }
   }
 }
 
 // zero_blocks blocks zero, zero_rows_of() rows each; the warps of the others take a stretch of T positions and a slice each.
-template <typename TI, typename TO, typename TOK, bool VECTOR, int PIECES>
+template <typename TI, typename TO, typename TOK, bool ALIGNED, int PIECES>
 __global__ void __launch_bounds__(EM_THREADS, PIECES == 1 ? 4 : 3)
 k_table_grad(const int2* order, const int2* span, const int* total, unsigned* counters, float* parts, const TOK* __restrict__ tokens, int ntokens,
              const TI* __restrict__ dY, long long ld, int vocab, int hidden, long long chunks, int slices, int zero_blocks, float scale, int add,
              TO* __restrict__ G, long long ldg) {
-  using Cols = Slice<TI, TO, VECTOR, PIECES>;
+  using Cols = Slice<TI, TO, ALIGNED, PIECES>;
   constexpr int N = Cols::N;
-  __shared__ uint4 ring[EM_WARPS][TG_DEPTH][32 * PIECES];
+  __shared__ uint4 ring[EM_WARPS][TG_DEPTH][Cols::WORDS];
+  __shared__ int skips[EM_WARPS][TG_DEPTH];
   // blocks that zero: in front where they need not wait, behind (where they fill the places that others leave) otherwise
   const bool early = ntokens <= TG_ZERO_EARLY;
   const int main_blocks = gridDim.x - zero_blocks, block = early ? (int)blockIdx.x - zero_blocks : (int)blockIdx.x;
   if (block < 0 || block >= main_blocks) {
     const int each = zero_rows_of(ntokens);
-    zero_rows<TO, TOK, VECTOR>((long long)(early ? blockIdx.x : block - main_blocks) * each, each, vocab, hidden, span, tokens, ntokens, early, G, ldg);
+    zero_rows<TO, TOK, ALIGNED>((long long)(early ? blockIdx.x : block - main_blocks) * each, each, vocab, hidden, span, tokens, ntokens, early, G, ldg);
     ptx::grid_wait();                       // (this kernel does not end before the one in front of it)
     return;
   }
@@ -548,7 +581,8 @@ k_table_grad(const int2* order, const int2* span, const int* total, unsigned* co
     for (int k = 0; k < N; ++k) sum[k] = 0.f;
   };
   // A window of 32 positions of the order: their tokens, and the rows that are fetched while they are summed.
-  uint4 (*slots)[32 * PIECES] = ring[threadIdx.x >> 5];
+  uint4 (*slots)[Cols::WORDS] = ring[threadIdx.x >> 5];
+  int* skip = skips[threadIdx.x >> 5];
   auto token_at = [&](int k) { return k < b ? order[k].y : -1; };
   auto row_at = [&](int k) { return k < b ? order[k].x : -1; };
   const int ahead = row_at(a + lane);
@@ -556,7 +590,7 @@ k_table_grad(const int2* order, const int2* span, const int* total, unsigned* co
 #pragma unroll
   for (int k = 0; k < TG_DEPTH; ++k) {
     const int i = __shfl_sync(0xffffffffu, ahead, k);
-    if (i >= 0) at.fetch(dY + (long long)i * ld, slots[k]);
+    if (i >= 0) at.fetch(dY + (long long)i * ld, slots[k], skip + k);
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
   int current = __shfl_sync(0xffffffffu, token, 0);
@@ -572,9 +606,9 @@ k_table_grad(const int2* order, const int2* span, const int* total, unsigned* co
       for (; k < end; ++k) {
         asm volatile("cp.async.wait_group %0;" :: "n"(TG_DEPTH - 1) : "memory");
         uint4* slot = slots[k % TG_DEPTH];
-        at.add(slot, sum);
+        at.add(slot, skip + k % TG_DEPTH, sum);
         const int i = __shfl_sync(0xffffffffu, row, k);
-        if (i >= 0) at.fetch(dY + (long long)i * ld, slot);
+        if (i >= 0) at.fetch(dY + (long long)i * ld, slot, skip + k % TG_DEPTH);
         asm volatile("cp.async.commit_group;" ::: "memory");
       }
       if (k >= m) break;
@@ -583,9 +617,9 @@ k_table_grad(const int2* order, const int2* span, const int* total, unsigned* co
       // the position that began it is summed now; the next change is looked for behind it
       asm volatile("cp.async.wait_group %0;" :: "n"(TG_DEPTH - 1) : "memory");
       uint4* slot = slots[k % TG_DEPTH];
-      at.add(slot, sum);
+      at.add(slot, skip + k % TG_DEPTH, sum);
       const int i = __shfl_sync(0xffffffffu, row, k);
-      if (i >= 0) at.fetch(dY + (long long)i * ld, slot);
+      if (i >= 0) at.fetch(dY + (long long)i * ld, slot, skip + k % TG_DEPTH);
       asm volatile("cp.async.commit_group;" ::: "memory");
       if (++k >= m) break;
     }
@@ -640,10 +674,11 @@ fira_status check_sizes(const std::string& who, int64_t count, int64_t vocab, in
 template <typename T, typename TOK>
 void run_lookup(const void* table, long long ld, const void* tokens, long long n, int vocab, int hidden, float scale, void* out, long long ld_out,
                 cudaStream_t st) {
-  const int width = 32 * rows::PER16<T>, slices = (hidden + width - 1) / width;
+  const bool aligned = rows::aligned16(table, ld, hidden, sizeof(T)) && rows::aligned16(out, ld_out, hidden, sizeof(T));
+  const int width = 32 * rows::PER16<T>, slices = (hidden + (aligned ? 0 : rows::PER16<T> - 1) + width - 1) / width;
   const long long units = (n + LK_ROWS - 1) / LK_ROWS * slices;
   const unsigned blocks = (unsigned)((units + EM_WARPS - 1) / EM_WARPS);
-  if (rows::aligned16(table, ld, hidden, sizeof(T)) && rows::aligned16(out, ld_out, hidden, sizeof(T)))
+  if (aligned)
     k_embedding<T, TOK, true><<<blocks, EM_THREADS, 0, st>>>((const T*)table, ld, (const TOK*)tokens, n, vocab, hidden, slices, scale, (T*)out, ld_out);
   else
     k_embedding<T, TOK, false><<<blocks, EM_THREADS, 0, st>>>((const T*)table, ld, (const TOK*)tokens, n, vocab, hidden, slices, scale, (T*)out, ld_out);
@@ -720,7 +755,7 @@ extern "C" fira_status fira_embedding(const void* table_dev, int64_t vocab, int6
       set_error("fira_embedding: pointers must be non-null and aligned to their elements"); return FIRA_ERR_INVALID_ARG;
     }
     const long long width = 32 * (16 / (long long)es);
-    if ((count + LK_ROWS - 1) / LK_ROWS * ((hidden + width - 1) / width) > 0x7fffffffll * EM_WARPS) { set_error("fira_embedding: too many elements in one call"); return FIRA_ERR_INVALID_ARG; }
+    if ((count + LK_ROWS - 1) / LK_ROWS * (hidden / width + 2) > 0x7fffffffll * EM_WARPS) { set_error("fira_embedding: too many elements in one call"); return FIRA_ERR_INVALID_ARG; }
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (dtype == FIRA_BF16) {
       if (token_bits == 32) run_lookup<__nv_bfloat16, int>(table_dev, ld, tokens_dev, count, (int)vocab, (int)hidden, scale, out_dev, ld_out, st);

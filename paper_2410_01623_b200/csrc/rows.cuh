@@ -1,5 +1,4 @@
-// Pieces of a row as fp32 registers: 16-byte accesses where rows start on 16-byte boundaries and their width is a
-// multiple of the piece, single elements otherwise.
+// Pieces of a row as fp32 registers, by 16-byte accesses on 16-byte boundaries, wherever the row begins.
 #pragma once
 #include "common.cuh"
 
@@ -81,6 +80,37 @@ __device__ __forceinline__ void store_vec(T* p, const float (&v)[N]) {
       }
     }
     reinterpret_cast<uint4*>(p)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// The 16 bytes that begin `skip` bytes behind the start of a, the last ones from b (0 <= skip < 16, the same in all lanes or not).
+__device__ __forceinline__ uint4 funnel16(const uint4& a, const uint4& b, int skip) {
+  unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  if (skip & 8) {
+#pragma unroll
+    for (int k = 0; k < 6; ++k) w[k] = w[k + 2];
+  }
+  if (skip & 4) {
+#pragma unroll
+    for (int k = 0; k < 5; ++k) w[k] = w[k + 1];
+  }
+  const int bits = (skip & 3) * 8;
+  return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+}
+// 16 bytes to `p`, which lies on a 16-byte boundary: those of its elements whose column, the first one being `col`, is in lo .. hi-1.
+template <typename T>
+__device__ __forceinline__ void store_between(T* p, const uint4& u, int col, int lo, int hi) {
+  constexpr int N = PER16<T>;
+  if (col >= lo && col + N <= hi) {
+    *reinterpret_cast<uint4*>(p) = u;
+  } else {
+    const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (col + e >= lo && col + e < hi) {
+        if constexpr (sizeof(T) == 4) reinterpret_cast<unsigned*>(p)[e] = w[e];
+        else reinterpret_cast<unsigned short*>(p)[e] = (unsigned short)(w[e / 2] >> (e & 1) * 16);
+      }
   }
 }
 
