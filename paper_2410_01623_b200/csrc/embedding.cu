@@ -28,6 +28,7 @@ constexpr int EM_SMS = 148;
 
 // ------------------------------------------------------------------------------------------------ lookup
 constexpr int LK_ROWS = 4;                 // rows of a warp in flight
+constexpr int LK_EACH = 2;                 // words of a thread
 
 template <typename TOK>
 __device__ __forceinline__ int token_at(const TOK* tokens, long long i, int vocab) {
@@ -35,54 +36,85 @@ __device__ __forceinline__ int token_at(const TOK* tokens, long long i, int voca
   return t >= 0 && t < vocab ? (int)t : -1;
 }
 
-// A warp takes LK_ROWS positions and a slice of the columns.  ALIGNED: all rows are whole 16-byte units on 16-byte boundaries.
-// Otherwise a lane has 16 aligned bytes of the output row and funnels them from two aligned words of the table, of which it
-// reads those that hold a byte of them.
-template <typename T, typename TOK, bool ALIGNED>
+// Wide rows of whole 16-byte units on 16-byte boundaries: a warp takes LK_ROWS positions and a slice of 32 units.
+// (131072 rows of 1024, bf16: 55 us; by k_embedding_words 64.  Of 64, fp32: 10.3 and 9.7.)
+template <typename T, typename TOK>
 __global__ void __launch_bounds__(EM_THREADS)
-k_embedding(const T* __restrict__ table, long long ld, const TOK* __restrict__ tokens, long long n, int vocab, int hidden, int slices,
-            float scale, T* __restrict__ out, long long ld_out) {
+k_embedding_rows(const T* __restrict__ table, long long ld, const TOK* __restrict__ tokens, long long n, int vocab, int hidden, int slices,
+                 float scale, T* __restrict__ out, long long ld_out) {
   constexpr int N = rows::PER16<T>;
-  const int lane = threadIdx.x & 31;
   const long long unit = (long long)blockIdx.x * EM_WARPS + (threadIdx.x >> 5);
   const long long i0 = unit / slices * LK_ROWS;
-  const int col0 = ((int)(unit % slices) * 32 + lane) * N;
-  if (i0 >= n) return;
+  const int col = ((int)(unit % slices) * 32 + (threadIdx.x & 31)) * N;
+  if (i0 >= n || col >= hidden) return;
   int t[LK_ROWS];
 #pragma unroll
   for (int u = 0; u < LK_ROWS; ++u) t[u] = i0 + u < n ? token_at(tokens, i0 + u, vocab) : -1;
-  uint4 a[LK_ROWS], b[LK_ROWS];
+  uint4 a[LK_ROWS];
+#pragma unroll
+  for (int u = 0; u < LK_ROWS; ++u) a[u] = t[u] >= 0 ? *reinterpret_cast<const uint4*>(table + (long long)t[u] * ld + col) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
   for (int u = 0; u < LK_ROWS; ++u) {
+    if (i0 + u >= n) break;
+    float2 v[N / 2];
+    rows::unpack<T>(a[u], v);
+#pragma unroll
+    for (int e = 0; e < N / 2; ++e) v[e] = rows::mul2(v[e], rows::both(scale));
+    *reinterpret_cast<uint4*>(out + (i0 + u) * ld_out + col) = rows::pack<T>(v);
+  }
+}
+
+// The output goes by words of 16 aligned bytes, `words` to a row, which are dealt to the threads in a row of their own, so that
+// rows of any width keep all lanes busy; a thread has LK_EACH of them.  ALIGNED: all rows are whole 16-byte units on
+// 16-byte boundaries.  Otherwise a word is funnelled from two aligned words of the table, of which those are read that
+// hold a byte of it.
+template <typename T, typename TOK, bool ALIGNED>
+__global__ void __launch_bounds__(EM_THREADS)
+k_embedding_words(const T* __restrict__ table, long long ld, const TOK* __restrict__ tokens, long long n, int vocab, int hidden, unsigned words,
+            float scale, T* __restrict__ out, long long ld_out) {
+  constexpr int N = rows::PER16<T>;
+  const long long first = (long long)blockIdx.x * (EM_THREADS * LK_EACH), row0 = first / words;
+  const unsigned word0 = (unsigned)(first - row0 * words);
+  uint4 a[LK_EACH], b[LK_EACH];
+  T* to[LK_EACH];                           // the word, and the column of its first element (hidden: none)
+  int col[LK_EACH], skip[LK_EACH];
+#pragma unroll
+  for (int u = 0; u < LK_EACH; ++u) {
+    const unsigned x = word0 + u * EM_THREADS + threadIdx.x, down = x / words;      // (words < 2^23: no overflow)
+    const long long i = row0 + down;
     a[u] = b[u] = make_uint4(0u, 0u, 0u, 0u);
-    const T* row = table + (long long)t[u] * ld;
+    col[u] = hidden; skip[u] = 0;
+    if (i >= n) continue;
+    const int t = token_at(tokens, i, vocab);
+    T* out_row = out + i * ld_out;
+    const T* row = table + (long long)max(t, 0) * ld;
+    col[u] = (int)(x - down * words) * N;
     if (ALIGNED) {
-      if (t[u] >= 0 && col0 < hidden) a[u] = *reinterpret_cast<const uint4*>(row + col0);
+      if (t >= 0) a[u] = *reinterpret_cast<const uint4*>(row + col[u]);
     } else {
-      const int col = col0 - (int)(((uintptr_t)(out + (i0 + u) * ld_out) & 15) / sizeof(T));
-      const uintptr_t from = (uintptr_t)(row + max(col, 0)), end = (uintptr_t)(row + min(col + N, hidden));      // the bytes that are wanted
-      const uintptr_t word = (uintptr_t)(row + col) & ~(uintptr_t)15;
-      if (t[u] >= 0 && from < end) {
+      col[u] -= (int)(((uintptr_t)out_row & 15) / sizeof(T));
+      const uintptr_t from = (uintptr_t)(row + max(col[u], 0)), end = (uintptr_t)(row + min(col[u] + N, hidden));     // the bytes that are wanted
+      const uintptr_t begin = (uintptr_t)(row + col[u]), word = begin & ~(uintptr_t)15;
+      skip[u] = (int)(begin & 15);
+      if (t >= 0 && from < end) {
         if (word + 16 > from) a[u] = *reinterpret_cast<const uint4*>(word);
         if (word + 16 < end) b[u] = *reinterpret_cast<const uint4*>(word + 16);
       }
     }
+    to[u] = out_row + col[u];
   }
 #pragma unroll
-  for (int u = 0; u < LK_ROWS; ++u) {
-    if (i0 + u >= n) break;
-    T* row = out + (i0 + u) * ld_out;
-    const int col = ALIGNED ? col0 : col0 - (int)(((uintptr_t)row & 15) / sizeof(T));
-    if (!ALIGNED) a[u] = rows::funnel16(a[u], b[u], (int)((uintptr_t)(table + (long long)t[u] * ld + col) & 15));
+  for (int u = 0; u < LK_EACH; ++u) {
+    if (!ALIGNED) a[u] = rows::funnel16(a[u], b[u], skip[u]);
     float2 v[N / 2];
     rows::unpack<T>(a[u], v);
 #pragma unroll
     for (int e = 0; e < N / 2; ++e) v[e] = rows::mul2(v[e], rows::both(scale));
     const uint4 w = rows::pack<T>(v);
     if (ALIGNED) {
-      if (col < hidden) *reinterpret_cast<uint4*>(row + col) = w;
+      if (col[u] < hidden) *reinterpret_cast<uint4*>(to[u]) = w;
     } else {
-      rows::store_between(row + col, w, col, 0, hidden);
+      if (col[u] < hidden) rows::store_between(to[u], w, col[u], 0, hidden);
     }
   }
 }
@@ -671,17 +703,23 @@ fira_status check_sizes(const std::string& who, int64_t count, int64_t vocab, in
   return FIRA_OK;
 }
 
+// The 16-byte words that a row of the output has a part of, at most.
+unsigned words_of(long long hidden, size_t size, bool aligned) { return (unsigned)((hidden * (long long)size + (aligned ? 0 : 16 - (long long)size) + 15) / 16); }
+
 template <typename T, typename TOK>
 void run_lookup(const void* table, long long ld, const void* tokens, long long n, int vocab, int hidden, float scale, void* out, long long ld_out,
                 cudaStream_t st) {
   const bool aligned = rows::aligned16(table, ld, hidden, sizeof(T)) && rows::aligned16(out, ld_out, hidden, sizeof(T));
-  const int width = 32 * rows::PER16<T>, slices = (hidden + (aligned ? 0 : rows::PER16<T> - 1) + width - 1) / width;
-  const long long units = (n + LK_ROWS - 1) / LK_ROWS * slices;
-  const unsigned blocks = (unsigned)((units + EM_WARPS - 1) / EM_WARPS);
-  if (aligned)
-    k_embedding<T, TOK, true><<<blocks, EM_THREADS, 0, st>>>((const T*)table, ld, (const TOK*)tokens, n, vocab, hidden, slices, scale, (T*)out, ld_out);
+  const unsigned words = words_of(hidden, sizeof(T), aligned);
+  const unsigned blocks = (unsigned)((n * words + EM_THREADS * LK_EACH - 1) / (EM_THREADS * LK_EACH));
+  if (aligned && words >= 96) {              // (the last slice of 32 leaves a quarter of the lanes idle at most)
+    const int slices = (int)((words + 31) / 32);
+    k_embedding_rows<T, TOK><<<(unsigned)(((n + LK_ROWS - 1) / LK_ROWS * slices + EM_WARPS - 1) / EM_WARPS), EM_THREADS, 0, st>>>(
+        (const T*)table, ld, (const TOK*)tokens, n, vocab, hidden, slices, scale, (T*)out, ld_out);
+  } else if (aligned)
+    k_embedding_words<T, TOK, true><<<blocks, EM_THREADS, 0, st>>>((const T*)table, ld, (const TOK*)tokens, n, vocab, hidden, words, scale, (T*)out, ld_out);
   else
-    k_embedding<T, TOK, false><<<blocks, EM_THREADS, 0, st>>>((const T*)table, ld, (const TOK*)tokens, n, vocab, hidden, slices, scale, (T*)out, ld_out);
+    k_embedding_words<T, TOK, false><<<blocks, EM_THREADS, 0, st>>>((const T*)table, ld, (const TOK*)tokens, n, vocab, hidden, words, scale, (T*)out, ld_out);
 }
 
 // Counts and lists may be above the default limit of shared memory: a setting per device and kernel.
@@ -754,8 +792,7 @@ extern "C" fira_status fira_embedding(const void* table_dev, int64_t vocab, int6
     if (!table_dev || !tokens_dev || !out_dev || (((uintptr_t)table_dev | (uintptr_t)out_dev) & (es - 1)) || ((uintptr_t)tokens_dev & (token_bits / 8 - 1))) {
       set_error("fira_embedding: pointers must be non-null and aligned to their elements"); return FIRA_ERR_INVALID_ARG;
     }
-    const long long width = 32 * (16 / (long long)es);
-    if ((count + LK_ROWS - 1) / LK_ROWS * (hidden / width + 2) > 0x7fffffffll * EM_WARPS) { set_error("fira_embedding: too many elements in one call"); return FIRA_ERR_INVALID_ARG; }
+    if (count * words_of(hidden, es, false) > 0x7fffffffll * EM_THREADS * LK_EACH) { set_error("fira_embedding: too many elements in one call"); return FIRA_ERR_INVALID_ARG; }
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (dtype == FIRA_BF16) {
       if (token_bits == 32) run_lookup<__nv_bfloat16, int>(table_dev, ld, tokens_dev, count, (int)vocab, (int)hidden, scale, out_dev, ld_out, st);
