@@ -331,12 +331,13 @@ k_token_split(const TOK* __restrict__ tokens, int n, int vocab, int blocks, int2
 // Block b sorts the entries of remainder b by row; a warp takes the tiles of a stretch.  Otherwise as k_token_order.
 __global__ void __launch_bounds__(ORD_MAX_THREADS)
 k_token_gather(const int2* entries, const int* counts, const int* fronts, int tiles, int vocab, int shift, int nrows, int2* order, int2* span, int* total) {
-  extern __shared__ unsigned shared[];      // counts [warps][nrows]
+  extern __shared__ unsigned shared[];      // counts [warps][nrows], lists [warps][ORD_LIST] of (position, token)
   __shared__ unsigned below_s[32], sum_s[32];
   ptx::grid_launch_next();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, threads = blockDim.x;
   const unsigned me = blockIdx.x;
   for (int i = threadIdx.x; i < warps * nrows; i += threads) shared[i] = 0;
+  __syncthreads();
   ptx::grid_wait();
   counts += (long long)me * tiles;
   fronts += (long long)me * tiles;
@@ -344,28 +345,41 @@ k_token_gather(const int2* entries, const int* counts, const int* fronts, int ti
   for (int t = threadIdx.x; t < tiles; t += threads) below += fronts[t];
   below = __reduce_add_sync(0xffffffffu, below);
   if (lane == 0) below_s[warp] = below;
-  __syncthreads();
   unsigned* mine = shared + warp * nrows;
+  int2* list = reinterpret_cast<int2*>(shared + ((warps * nrows + 1) & ~1)) + warp * ORD_LIST;
   const int per_warp = (tiles + warps - 1) / warps, t0 = min(tiles, warp * per_warp), t1 = min(tiles, t0 + per_warp);
-  for (int t = t0; t < t1; ++t) {
-    const int c = counts[t];
-    const int2* e = entries + (long long)t * ORD_TILE + fronts[t];
-    for (int k = lane; k < c; k += 32) atomicAdd(&mine[(unsigned)e[k].y >> shift], 1u);
-  }
+  // The entries of this warp's tiles one behind another, 32 at a time: f(whether this lane has one, its number, its place).
+  auto each = [&](auto f) {
+    int seen = 0;
+    for (int t = t0; t < t1; t += 32) {
+      const int here = min(32, t1 - t), c = lane < here ? counts[t + lane] : 0;
+      const int at = lane < here ? (t + lane) * ORD_TILE + fronts[t + lane] : 0;       // (tiles * ORD_TILE is about n)
+      const int inclusive = (int)warp_inclusive((unsigned)c), all = __shfl_sync(0xffffffffu, inclusive, 31);
+      for (int k = lane; k - lane < all; k += 32) {
+        int j = 0;
+        for (int i = 0; i + 1 < here; ++i) j += k >= __shfl_sync(0xffffffffu, inclusive, i);
+        const int begins = __shfl_sync(0xffffffffu, at - (inclusive - c), j);
+        f(k < all, seen + k, begins + k);
+      }
+      seen += all;
+    }
+  };
+  each([&](bool in, int k, int at) {
+    if (in) {
+      const int2 x = entries[at];
+      atomicAdd(&mine[(unsigned)x.y >> shift], 1u);
+      if (k < ORD_LIST) list[k] = x;
+    }
+  });
   __syncthreads();
   unsigned front = 0;
   for (int w = 0; w < warps; ++w) front += below_s[w];
   const unsigned end = row_fronts(shared, warps, nrows, front, shift, me, vocab, span, sum_s);
   if (me == gridDim.x - 1 && threadIdx.x == 0) *total = (int)end;
-  for (int t = t0; t < t1; ++t) {
-    const int c = counts[t];
-    const int2* e = entries + (long long)t * ORD_TILE + fronts[t];
-    for (int k = 0; k < c; k += 32) {
-      const bool in = k + lane < c;
-      const int2 x = in ? e[k + lane] : make_int2(0, 0);
-      place_entries(in, (unsigned)x.y >> shift, x.x, x.y, mine, order);
-    }
-  }
+  each([&](bool in, int k, int at) {
+    const int2 x = !in ? make_int2(0, 0) : k < ORD_LIST ? list[k] : entries[at];
+    place_entries(in, (unsigned)x.y >> shift, x.x, x.y, mine, order);
+  });
 }
 
 // ------------------------------------------------------------------------------------------------ sums of the rows
@@ -723,15 +737,17 @@ void run_lookup(const void* table, long long ld, const void* tokens, long long n
 }
 
 // Counts and lists may be above the default limit of shared memory: a setting per device and kernel.
+size_t order_smem(int warps, int nrows) { return (size_t)((warps * nrows + 1) & ~1) * sizeof(unsigned) + (size_t)warps * ORD_LIST * sizeof(int2); }
+
 template <typename TOK>
 cudaError_t run_split(const TablePlan& p, const void* tokens, int n, int vocab, char* work, cudaStream_t st) {
-  const size_t smem = (size_t)32 * p.blocks * sizeof(unsigned), gather = (size_t)(p.threads / 32) * p.nrows * sizeof(unsigned);
+  const size_t smem = (size_t)32 * p.blocks * sizeof(unsigned), gather = order_smem(p.threads / 32, p.nrows);
   if (smem > 47 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(k_token_split<TOK>, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * ORD_SPLIT_BLOCKS * 4);
     if (e != cudaSuccess) return e;
   }
   if (gather > 47 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(k_token_gather, cudaFuncAttributeMaxDynamicSharedMemorySize, ORD_MAX_THREADS / 32 * ORD_MAX_ROWS * 4);
+    const cudaError_t e = cudaFuncSetAttribute(k_token_gather, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)order_smem(ORD_MAX_THREADS / 32, ORD_MAX_ROWS));
     if (e != cudaSuccess) return e;
   }
   int2* entries = (int2*)(work + p.off_entries);
@@ -747,10 +763,9 @@ cudaError_t run_split(const TablePlan& p, const void* tokens, int n, int vocab, 
 template <typename TOK, bool VECTOR>
 cudaError_t run_order(const TablePlan& p, const void* tokens, int n, int vocab, char* work, cudaStream_t st) {
   if (p.tiles) return run_split<TOK>(p, tokens, n, vocab, work, st);
-  auto bytes = [](int warps, int nrows) { return (size_t)((warps * nrows + 1) & ~1) * sizeof(unsigned) + (size_t)warps * ORD_LIST * sizeof(int2); };
-  const size_t smem = bytes(p.threads / 32, p.nrows);
+  const size_t smem = order_smem(p.threads / 32, p.nrows);
   if (smem > 47 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(k_token_order<TOK, VECTOR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes(ORD_MAX_THREADS / 32, ORD_MAX_ROWS));
+    const cudaError_t e = cudaFuncSetAttribute(k_token_order<TOK, VECTOR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)order_smem(ORD_MAX_THREADS / 32, ORD_MAX_ROWS));
     if (e != cudaSuccess) return e;
   }
   k_token_order<TOK, VECTOR><<<p.blocks, p.threads, smem, st>>>((const TOK*)tokens, n, vocab, p.shift, p.nrows, (int2*)work, (int2*)(work + p.off_span),
