@@ -228,28 +228,31 @@ k_token_order(const TOK* __restrict__ tokens, int n, int vocab, int shift, int n
   const int s0 = min(steps, warp * per_warp), s1 = min(steps, s0 + per_warp);
   unsigned below = 0;
   int listed = 0;                           // entries of this warp, whether the list holds them or not
-  unsigned next[4];
-  load_tokens<TOK, VECTOR>(tokens, s0 * ORD_STEP + lane * 4, s0 < s1 ? n : 0, vocab, next);
-  for (int s = s0; s < s1; ++s) {
-    unsigned t[4], home[4];                 // home of a position without a token: no block's
+  constexpr int AHEAD = 4;                  // steps whose tokens are on their way at once
+  for (int first = s0; first < s1; first += AHEAD) {
+    unsigned t[AHEAD][4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      t[j] = next[j];
-      home[j] = t[j] == 0xffffffffu ? t[j] : t[j] & mask;
-      below += home[j] < me;
-    }
-    if (s + 1 < s1) load_tokens<TOK, VECTOR>(tokens, (s + 1) * ORD_STEP + lane * 4, n, vocab, next);
-    if (!__any_sync(0xffffffffu, home[0] == me || home[1] == me || home[2] == me || home[3] == me)) continue;
+    for (int u = 0; u < AHEAD; ++u) load_tokens<TOK, VECTOR>(tokens, (first + u) * ORD_STEP + lane * 4, first + u < s1 ? n : 0, vocab, t[u]);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const unsigned found = __ballot_sync(0xffffffffu, home[j] == me);
-      if (home[j] == me) {
-        const unsigned r = t[j] >> shift;
-        atomicAdd(&mine[r], 1u);
-        const int k = listed + __popc(found & ((1u << lane) - 1));
-        if (k < ORD_LIST) list[k] = make_int2(s * ORD_STEP + lane * 4 + j, (int)r);
+    for (int u = 0; u < AHEAD; ++u) {
+      unsigned home[4];                     // of a position without a token: no block's
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        home[j] = t[u][j] == 0xffffffffu ? t[u][j] : t[u][j] & mask;
+        below += home[j] < me;
       }
-      listed += __popc(found);
+      if (!__any_sync(0xffffffffu, home[0] == me || home[1] == me || home[2] == me || home[3] == me)) continue;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const unsigned found = __ballot_sync(0xffffffffu, home[j] == me);
+        if (home[j] == me) {
+          const unsigned r = t[u][j] >> shift;
+          atomicAdd(&mine[r], 1u);
+          const int k = listed + __popc(found & ((1u << lane) - 1));
+          if (k < ORD_LIST) list[k] = make_int2((first + u) * ORD_STEP + lane * 4 + j, (int)r);
+        }
+        listed += __popc(found);
+      }
     }
   }
   below = __reduce_add_sync(0xffffffffu, below);
