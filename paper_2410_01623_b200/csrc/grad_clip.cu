@@ -14,7 +14,7 @@
 
 #include <algorithm>
 
-#include "common.cuh"
+#include "rows.cuh"
 #include "tc_ptx.cuh"
 
 namespace fira {
@@ -51,15 +51,6 @@ struct GradTable {
   int count, tiles;
 };
 
-__device__ __forceinline__ void unpack8(const uint4& u, float (&v)[8]) {
-  const unsigned w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-
 // Where chunk c of the tensor starts in G and in out, and how many elements it has.
 struct Place { long long at, out_at; int len; };
 __device__ __forceinline__ Place place(const GradEntry& t, long long c, long long row0, unsigned col0, unsigned local) {
@@ -86,12 +77,9 @@ __device__ __forceinline__ void load_chunk(const GradEntry& t, const Place& p, f
   for (int e = 0; e < 8; ++e) v[e] = 0.f;
   if (p.len == 8) {
     if (t.bf16) {
-      unpack8(*reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(t.g) + p.at), v);
+      rows::load_vec<__nv_bfloat16, 8>(static_cast<const __nv_bfloat16*>(t.g) + p.at, v);
     } else {
-      const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(t.g) + p.at);
-      const float4 a = q[0], b = q[1];
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+      rows::load_vec<float, 8>(static_cast<const float*>(t.g) + p.at, v);
     }
   } else {
 #pragma unroll
@@ -102,20 +90,8 @@ __device__ __forceinline__ void load_chunk(const GradEntry& t, const Place& p, f
 
 __device__ __forceinline__ void store_chunk(const GradEntry& t, const Place& p, const float (&v)[8]) {
   if (p.len == 8) {
-    if (t.out_bf16) {
-      uint4 u;
-      unsigned* w = reinterpret_cast<unsigned*>(&u);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        w[i] = *reinterpret_cast<const unsigned*>(&h);
-      }
-      *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(t.o) + p.out_at) = u;
-    } else {
-      float4* q = reinterpret_cast<float4*>(static_cast<float*>(t.o) + p.out_at);
-      q[0] = make_float4(v[0], v[1], v[2], v[3]);
-      q[1] = make_float4(v[4], v[5], v[6], v[7]);
-    }
+    if (t.out_bf16) rows::store_vec<__nv_bfloat16, 8>(static_cast<__nv_bfloat16*>(t.o) + p.out_at, v);
+    else rows::store_vec<float, 8>(static_cast<float*>(t.o) + p.out_at, v);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
@@ -194,12 +170,8 @@ __device__ __forceinline__ void load_whole(const void* g, long long first, uint6
 }
 template <int W>
 __device__ __forceinline__ void unpack_whole(const uint4& u, float* v) {
-  const unsigned w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if (W == 8) v[k] = __uint_as_float(w[k]);
-    else { v[2 * k] = __uint_as_float(w[k] << 16); v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u); }
-  }
+  if constexpr (W == 8) rows::unpack<float>(u, v);
+  else rows::unpack<__nv_bfloat16>(u, v);
 }
 constexpr int GC_ELEMS = GC_UNROLL * GC_CHUNK;     // of a thread in a tile
 
@@ -351,26 +323,20 @@ int launches_for(int count) { return (count + GC_MANY - 1) / GC_MANY; }
 fira_status check_list(const char* who, int32_t count, const fira_grad_desc* descs, const void* const* G_dev, void* const* out_dev) {
   const std::string name(who);
   if (count <= 0 || !descs || !G_dev) { set_error(name + ": null argument or empty list"); return FIRA_ERR_INVALID_ARG; }
+  auto refuse = [&](int i, const char* why) { set_error(name + ": tensor " + std::to_string(i) + ": " + why); return FIRA_ERR_INVALID_ARG; };
   for (int base = 0; base < count; base += GC_MANY) {
     long long tiles = 0;
     for (int i = base; i < std::min(count, base + GC_MANY); ++i) {
       const fira_grad_desc& d = descs[i];
-      const std::string at = name + ": tensor " + std::to_string(i) + ": ";
-      if (d.rows < 0 || d.cols < 0) { set_error(at + "negative size"); return FIRA_ERR_INVALID_ARG; }
-      if (d.rows > 1 && ((d.ld != 0 && d.ld < d.cols) || (out_dev && d.out_ld != 0 && d.out_ld < d.cols))) {
-        set_error(at + "ld below the width"); return FIRA_ERR_INVALID_ARG;
-      }
-      if ((d.dtype != FIRA_F32 && d.dtype != FIRA_BF16) || (out_dev && d.out_dtype != FIRA_F32 && d.out_dtype != FIRA_BF16)) {
-        set_error(at + "unknown dtype"); return FIRA_ERR_INVALID_ARG;
-      }
+      if (d.rows < 0 || d.cols < 0) return refuse(i, "negative size");
+      if (d.rows > 1 && ((d.ld != 0 && d.ld < d.cols) || (out_dev && d.out_ld != 0 && d.out_ld < d.cols))) return refuse(i, "ld below the width");
+      if ((d.dtype != FIRA_F32 && d.dtype != FIRA_BF16) || (out_dev && d.out_dtype != FIRA_F32 && d.out_dtype != FIRA_BF16)) return refuse(i, "unknown dtype");
       if (d.rows == 0 || d.cols == 0) continue;
-      if (d.rows > (1ll << 40) || d.cols > (1ll << 40) || d.rows > (1ll << 42) / d.cols || (d.rows > 1 && (d.cols >= (1ll << 31) - GC_TILE || d.ld > (1ll << 40) || d.out_ld > (1ll << 40)))) {
-        set_error(at + "too large"); return FIRA_ERR_INVALID_ARG;
-      }
+      const long long pitch = std::max<long long>({d.cols, d.rows > 1 ? d.ld : 0, d.rows > 1 && out_dev ? d.out_ld : 0});
+      if (d.rows > (1ll << 40) || d.cols > (1ll << 40) || d.rows > (1ll << 42) / pitch || (d.rows > 1 && d.cols >= (1ll << 31) - GC_TILE)) return refuse(i, "too large");
       const size_t es = d.dtype == FIRA_BF16 ? 2 : 4, os = d.out_dtype == FIRA_BF16 ? 2 : 4;
-      if (!G_dev[i] || ((uintptr_t)G_dev[i] & (es - 1)) || (out_dev && (!out_dev[i] || ((uintptr_t)out_dev[i] & (os - 1))))) {
-        set_error(at + "pointers must be non-null and aligned to their elements"); return FIRA_ERR_INVALID_ARG;
-      }
+      if (!G_dev[i] || ((uintptr_t)G_dev[i] & (es - 1)) || (out_dev && (!out_dev[i] || ((uintptr_t)out_dev[i] & (os - 1)))))
+        return refuse(i, "pointers must be non-null and aligned to their elements");
       // every element a chunk of its own is the most that a tensor takes
       tiles += (d.rows * d.cols + GC_TILE - 1) / GC_TILE;
     }

@@ -158,6 +158,61 @@ def test_large_batches(n, hidden, dtype, kind):
     check_grad(tokens, dY, vocab, 1.0, fb.embedding_grad(tokens, dY, vocab))
 
 
+@pytest.mark.parametrize("n,vocab,hidden", [(20000, 200003, 16), (20000, 600000, 8), (16384, 3000, 33), (16385, 3000, 33), (1 << 20, 40, 8), (70000, 32000, 3),
+                                            (40, 30, 20000), (40, 30, 20001)])
+@pytest.mark.parametrize("dtype,kind", [(F32, "zipf"), (BF16, "mixed")])
+def test_large_vocabularies_batches_and_widths(n, vocab, hidden, dtype, kind):
+    """More remainders than the smallest number, more than the two launches take, batches on both sides of the border between one
+    and two launches, a batch of a million positions, rows of many slices."""
+    gen = torch.Generator().manual_seed(n + hidden)
+    tokens = make_tokens(gen, kind, n, vocab).cuda()
+    dY = torch.randn(n, hidden, generator=gen).to(dtype).cuda()
+    G = fb.embedding_grad(tokens, dY, vocab)
+    check_grad(tokens, dY, vocab, 1.0, G)
+    Y = fb.embedding(G, tokens)
+    ok = (tokens.long() >= 0) & (tokens.long() < vocab)
+    assert torch.equal(Y, torch.where(ok[:, None], G[tokens.long().clamp(0, vocab - 1)], 0.0).to(dtype))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shift,gshift", [(0, 1), (1, 0), (1, 1), (1, 2), (3, 1)])
+@pytest.mark.parametrize("hidden", [24, 33, 300, 1023])
+def test_rows_that_begin_anywhere(dtype, shift, gshift, hidden):
+    """dY, G, table and output each begin elsewhere between two 16-byte boundaries; guards around G and the output stay."""
+    gen = torch.Generator().manual_seed(hidden)
+    n, vocab = 500, 41
+    tokens = make_tokens(gen, "mixed", n, vocab).cuda()
+    dY = torch.randn(n * hidden + 8, generator=gen).to(dtype).cuda()[shift:shift + n * hidden].view(n, hidden)
+    buf = torch.full((vocab * hidden + 16,), 5.0, dtype=dtype, device="cuda")
+    G = buf[gshift:gshift + vocab * hidden].view(vocab, hidden)
+    fb.embedding_grad(tokens, dY, vocab, out=G)
+    check_grad(tokens, dY, vocab, 1.0, G)
+    assert bool((buf[:gshift] == 5.0).all()) and bool((buf[gshift + vocab * hidden:] == 5.0).all())
+    outs = torch.full((n * hidden + 16,), 5.0, dtype=dtype, device="cuda")
+    Y = outs[shift:shift + n * hidden].view(n, hidden)
+    fb.embedding(G, tokens, out=Y)
+    ok = (tokens.long() >= 0) & (tokens.long() < vocab)
+    assert torch.equal(Y, torch.where(ok[:, None], G[tokens.long().clamp(0, vocab - 1)], 0.0).to(dtype))
+    assert bool((outs[:shift] == 5.0).all()) and bool((outs[shift + n * hidden:] == 5.0).all())
+
+
+def test_two_calls_at_once_on_two_streams():
+    gen = torch.Generator().manual_seed(16)
+    calls = []
+    for k in range(2):
+        tokens = make_tokens(gen, "zipf", 30000, 4000).cuda()
+        dY = torch.randn(30000, 96, generator=gen).cuda()
+        calls.append((tokens, dY, torch.empty(4000, 96, device="cuda"), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for tokens, dY, G, stream in calls:
+            with torch.cuda.stream(stream):
+                fb.embedding_grad(tokens, dY, 4000, out=G)
+    torch.cuda.synchronize()
+    for tokens, dY, G, _ in calls:
+        check_grad(tokens, dY, 4000, 1.0, G)
+
+
 def test_no_positions():
     empty = torch.zeros(0, dtype=torch.int64, device="cuda")
     G = torch.full((1000, 40), 3.0, device="cuda")

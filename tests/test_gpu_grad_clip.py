@@ -196,6 +196,38 @@ def test_captured_and_replayed_on_another_stream():
     assert abs(float(fb.grad_norm(Gs)) - 0.5) <= 0.5 * (NORM + SCALE + U)
 
 
+@pytest.mark.parametrize("count", [60, 500])
+def test_a_long_list_captured_and_replayed(count):
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    Gs = [torch.randn(1 + 53 * i, generator=gen, device="cuda").to([torch.float32, torch.bfloat16][i % 2]) for i in range(count)]
+    out = [torch.empty_like(g) for g in Gs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        norm, scale = fb.clip_grads(Gs, 1.0, out=out)
+    for _ in range(2):
+        for g in Gs:
+            g.mul_(0.5)
+        graph.replay()
+        check(Gs, out, norm, scale, 1.0)
+
+
+def test_two_calls_at_once_on_two_streams():
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    lists = [[torch.randn(n, generator=gen, device="cuda") for n in (2_000_000, 333)] for _ in range(2)]
+    outs = [[torch.empty_like(g) for g in Gs] for Gs in lists]
+    streams = [torch.cuda.Stream() for _ in lists]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        got = []
+        for Gs, out, stream in zip(lists, outs, streams):
+            with torch.cuda.stream(stream):
+                got.append(fb.clip_grads(Gs, 2.0, out=out))
+    torch.cuda.synchronize()
+    for Gs, out, (norm, scale) in zip(lists, outs, got):
+        check(Gs, out, norm, scale, 2.0)
+
+
 def test_many_elements_in_one_tensor():
     """Offsets beyond 2^32 bytes, and beyond 2^31 elements."""
     n = (1 << 31) + 12345

@@ -146,6 +146,38 @@ def test_accumulation(grad_dtype, rms):
     check_backward(dY, x, gain, mean, rstd, rms, *got, old=old)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shifts", [(1, 1, 1, 1), (0, 1, 0, 1), (3, 3, 2, 3), (1, 2, 3, 0)])
+@pytest.mark.parametrize("hidden", [16, 37, 520, 4097])
+def test_rows_that_begin_anywhere(dtype, shifts, hidden):
+    """x, y, dY and dX each begin elsewhere between two 16-byte boundaries, alike or not; what lies around them stays."""
+    rows = 37
+    x, dY, gain, bias = inputs(rows, hidden, dtype, F32, seed=hidden)
+    flat = [torch.full((rows * hidden + 16,), 6.0, dtype=dtype, device="cuda") for _ in range(4)]
+    xs, ys, dys, dxs = [f[k:k + rows * hidden].view(rows, hidden) for f, k in zip(flat, shifts)]
+    xs.copy_(x)
+    dys.copy_(dY)
+    y, mean, rstd = fb.layer_norm(xs, gain, bias, out=ys)
+    check_forward(x, gain, bias, 1e-5, False, y, mean, rstd)
+    check_backward(dY, x, gain, mean, rstd, False, *fb.layer_norm_grad(dys, xs, gain, mean, rstd, out=dxs))
+    assert torch.equal(xs, x) and torch.equal(dys, dY)
+    for f, k in zip(flat, shifts):
+        assert bool((f[:k] == 6.0).all()) and bool((f[k + rows * hidden:] == 6.0).all())
+
+
+def test_backward_pass_without_the_bias_gradient():
+    x, dY, gain, bias = inputs(200, 72, F32, F32)
+    y, mean, rstd = fb.layer_norm(x, gain, bias)
+    want = fb.layer_norm_grad(dY, x, gain, mean, rstd)
+    dX, dgain = torch.empty_like(x), torch.empty_like(gain)
+    L = fb.lib()
+    work = torch.empty(L.fira_layer_norm_grad_work_bytes(200, 72, 0), dtype=torch.uint8, device="cuda")
+    fb.check(L.fira_layer_norm_grad(dY.data_ptr(), 0, x.data_ptr(), 0, 0, 200, 72, gain.data_ptr(), 0, mean.data_ptr(), rstd.data_ptr(),
+                                    dX.data_ptr(), 0, dgain.data_ptr(), None, 0, 0, work.data_ptr(), work.nbytes,
+                                    torch.cuda.current_stream().cuda_stream))
+    assert torch.equal(dX, want[0]) and torch.equal(dgain, want[1])
+
+
 def test_more_dimensions_and_no_rows():
     x, dY, gain, bias = inputs(60, 40, F32, F32)
     y, mean, rstd = fb.layer_norm(x.view(3, 20, 40), gain, bias)

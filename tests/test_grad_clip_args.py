@@ -38,7 +38,8 @@ def test_max_norm_must_be_positive(lib, max_norm):
 
 @pytest.mark.parametrize("desc", [
     D(-1, 8, 0, 0, 0, 0), D(1, -8, 0, 0, 0, 0), D(2, 8, 7, 0, 0, 0), D(1, 8, 0, 0, 2, 0),
-    D(1 << 41, 1, 0, 0, 0, 0), D(1, 1 << 41, 0, 0, 0, 0), D(1 << 22, 1 << 22, 0, 0, 0, 0), D(2, 1 << 31, 0, 0, 0, 0)])
+    D(1 << 41, 1, 0, 0, 0, 0), D(1, 1 << 41, 0, 0, 0, 0), D(1 << 22, 1 << 22, 0, 0, 0, 0), D(2, 1 << 31, 0, 0, 0, 0),
+    D(1 << 30, 4, 1 << 20, 0, 0, 0), D(1 << 40, 1, 1 << 40, 0, 0, 0)])
 @pytest.mark.parametrize("norm_only", [False, True])
 def test_bad_tensors_are_refused(lib, desc, norm_only):
     assert call(lib, [D(1, 8, 0, 0, 0, 0), desc], norm_only=norm_only) == INVALID
