@@ -40,10 +40,16 @@ struct GradEntry {
   long long chunks;         // of the whole tensor
   int tile_start;           // tiles of the tensors in front of it
   unsigned char bf16, out_bf16;
-  unsigned char single;     // a chunk is one element: rows that do not start on 16-byte boundaries
-  unsigned char pitched;
-  long long whole;          // tiles from the first on that are GC_TILE whole chunks in a row (the others go chunk by chunk)
+  unsigned char single;     // a chunk is one element: where G and out do not begin alike
+  unsigned char pitched : 1;
+  unsigned char shift : 7;  // elements from a 16-byte boundary to the first one of a row, alike in G and out and in all rows
+  long long whole;          // tiles from the first on that end within the tensor (the others go chunk by chunk)
 };
+// A tile of GC_TILE whole chunks in a row: not the first one of a tensor that begins between two boundaries.
+__device__ __forceinline__ bool is_whole(const GradEntry& t, int tile) {
+  const int i = tile - t.tile_start;
+  return i < t.whole && (i > 0 || t.shift == 0);
+}
 
 template <int CAP>
 struct GradTable {
@@ -55,20 +61,20 @@ struct GradTable {
 struct Place { long long at, out_at; int len; };
 __device__ __forceinline__ Place place(const GradEntry& t, long long c, long long row0, unsigned col0, unsigned local) {
   const int w = t.single ? 1 : GC_CHUNK;
-  Place p;
+  long long col, row = 0;
   if (!t.pitched) {
-    p.at = p.out_at = c * w;
-    const long long left = t.n - p.at;
-    p.len = left < w ? (int)left : w;
+    col = c * w - t.shift;
   } else {
-    const unsigned per_row = (unsigned)((t.n + w - 1) / w);
+    const unsigned per_row = (unsigned)((t.n + t.shift + w - 1) / w);
     const unsigned x = col0 + local, down = x / per_row;      // col0 < per_row < 2^31, local < 2^11: no overflow
-    const long long col = (long long)(x - down * per_row) * w;
-    p.at = (row0 + down) * t.ld + col;
-    p.out_at = (row0 + down) * t.out_ld + col;
-    const long long left = t.n - col;
-    p.len = left < w ? (int)left : w;
+    col = (long long)(x - down * per_row) * w - t.shift;
+    row = row0 + down;
   }
+  const long long from = col < 0 ? 0 : col, to = col + w < t.n ? col + w : t.n;
+  Place p;
+  p.at = row * t.ld + from;
+  p.out_at = row * t.out_ld + from;
+  p.len = (int)(to - from);
   return p;
 }
 
@@ -139,7 +145,7 @@ __device__ __forceinline__ Tile open_tile(const GradEntry* t, int q, int tile) {
   x.row0 = 0; x.col0 = 0;
   if (t[q].pitched) {
     const int w = t[q].single ? 1 : GC_CHUNK;
-    const long long per_row = (t[q].n + w - 1) / w;
+    const long long per_row = (t[q].n + t[q].shift + w - 1) / w;
     x.row0 = x.first / per_row;
     x.col0 = (unsigned)(x.first - x.row0 * per_row);
   }
@@ -163,8 +169,8 @@ __device__ __forceinline__ void load_tile(const GradEntry* tab, const Tile& x, P
 
 // Whole tiles: 16 bytes per thread and load, W of them (4: bf16, 8: fp32).
 template <int W>
-__device__ __forceinline__ void load_whole(const void* g, long long first, uint64_t pol, uint4 (&u)[W]) {
-  const uint4* p = static_cast<const uint4*>(g) + first * (W / GC_UNROLL) + threadIdx.x;
+__device__ __forceinline__ void load_whole(const GradEntry& t, long long first, uint64_t pol, uint4 (&u)[W]) {
+  const uint4* p = reinterpret_cast<const uint4*>(static_cast<const char*>(t.g) - t.shift * (W == 8 ? 4 : 2)) + first * (W / GC_UNROLL) + threadIdx.x;
 #pragma unroll
   for (int i = 0; i < W; ++i) u[i] = load16(p + i * GC_THREADS, pol);
 }
@@ -192,18 +198,18 @@ __device__ __forceinline__ double squares(const float (&v)[GC_ELEMS]) {
   return d;
 }
 template <int W>
-__device__ __forceinline__ double whole_squares(const void* g, long long first, uint64_t pol) {
+__device__ __forceinline__ double whole_squares(const GradEntry& t, long long first, uint64_t pol) {
   uint4 u[W];
-  load_whole<W>(g, first, pol, u);
+  load_whole<W>(t, first, pol, u);
   float v[GC_ELEMS];
 #pragma unroll
   for (int i = 0; i < W; ++i) unpack_whole<W>(u[i], v + i * (GC_ELEMS / W));
   return squares(v);
 }
 template <int W, bool OUT_BF16>
-__device__ __forceinline__ void whole_scale(const void* g, void* o, long long first, float scale, uint64_t pol) {
+__device__ __forceinline__ void whole_scale(const GradEntry& t, long long first, float scale, uint64_t pol) {
   uint4 u[W];
-  load_whole<W>(g, first, pol, u);
+  load_whole<W>(t, first, pol, u);
 #pragma unroll
   for (int i = 0; i < W; ++i) {
     constexpr int N = GC_ELEMS / W;
@@ -212,13 +218,13 @@ __device__ __forceinline__ void whole_scale(const void* g, void* o, long long fi
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] *= scale;
     // the 16 bytes that were read, seen as elements of the tensor
-    const long long at = (first * (W / GC_UNROLL) + i * GC_THREADS + threadIdx.x) * N;
+    const long long at = (first * (W / GC_UNROLL) + i * GC_THREADS + threadIdx.x) * N - t.shift;
     if constexpr (OUT_BF16) {
-      __nv_bfloat16* q = static_cast<__nv_bfloat16*>(o) + at;
+      __nv_bfloat16* q = static_cast<__nv_bfloat16*>(t.o) + at;
       if constexpr (N == 8) store16(q, make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])), pol);
       else store8(q, pack2(v[0], v[1]), pack2(v[2], v[3]), pol);
     } else {
-      float* q = static_cast<float*>(o) + at;
+      float* q = static_cast<float*>(t.o) + at;
 #pragma unroll
       for (int e = 0; e < N; e += 4)
         store16(q + e, make_uint4(__float_as_uint(v[e]), __float_as_uint(v[e + 1]), __float_as_uint(v[e + 2]), __float_as_uint(v[e + 3])), pol);
@@ -248,10 +254,10 @@ k_grad_squares(const __grid_constant__ GradTable<CAP> tab, double* __restrict__ 
   for (int tile = blockIdx.x; tile < tab.tiles; tile += gridDim.x) {
     while (q + 1 < tab.count && tile >= tab.t[q + 1].tile_start) ++q;
     const GradEntry& t = tab.t[q];
-    if (tile - t.tile_start < t.whole) {
+    if (is_whole(t, tile)) {
       const uint64_t pol = tile >= kept ? again : once;
       const long long first = (long long)(tile - t.tile_start) * GC_TILE;
-      total += t.bf16 ? whole_squares<4>(t.g, first, pol) : whole_squares<8>(t.g, first, pol);
+      total += t.bf16 ? whole_squares<4>(t, first, pol) : whole_squares<8>(t, first, pol);
     } else {
       Place p[GC_UNROLL];
       float v[GC_UNROLL][8];
@@ -295,14 +301,14 @@ k_grad_scale(const __grid_constant__ GradTable<CAP> tab, const double* sums, int
   for (int tile = tab.tiles - 1 - (int)blockIdx.x; tile >= 0; tile -= gridDim.x) {
     while (tile < tab.t[q].tile_start) --q;
     const GradEntry& t = tab.t[q];
-    if (tile - t.tile_start < t.whole) {
+    if (is_whole(t, tile)) {
       const long long first = (long long)(tile - t.tile_start) * GC_TILE;
       if (t.bf16) {
-        if (t.out_bf16) whole_scale<4, true>(t.g, t.o, first, scale, once);
-        else whole_scale<4, false>(t.g, t.o, first, scale, once);
+        if (t.out_bf16) whole_scale<4, true>(t, first, scale, once);
+        else whole_scale<4, false>(t, first, scale, once);
       } else {
-        if (t.out_bf16) whole_scale<8, true>(t.g, t.o, first, scale, once);
-        else whole_scale<8, false>(t.g, t.o, first, scale, once);
+        if (t.out_bf16) whole_scale<8, true>(t, first, scale, once);
+        else whole_scale<8, false>(t, first, scale, once);
       }
     } else {
       Place p[GC_UNROLL];
@@ -384,10 +390,13 @@ void fill(GradTable<CAP>& tab, int base, int n, const fira_grad_desc* descs, con
     t.ld = ld; t.out_ld = out_ld;
     t.pitched = ld != d.cols || out_ld != d.cols;
     t.n = t.pitched ? d.cols : d.rows * d.cols;
-    t.single = (((uintptr_t)t.g | (uintptr_t)t.o) & 15) != 0 || (t.pitched && ((ld * es | out_ld * os) & 15) != 0);
+    // elements behind a 16-byte boundary: bf16 has the longer way between two of them
+    const size_t shift = t.out_bf16 ? ((uintptr_t)t.o & 15) / 2 : t.bf16 ? ((uintptr_t)t.g & 15) / 2 : ((uintptr_t)t.g & 15) / 4;
+    t.single = (((uintptr_t)t.g - shift * es) & 15) != 0 || (((uintptr_t)t.o - shift * os) & 15) != 0 || (t.pitched && ((ld * es | out_ld * os) & 15) != 0);
+    t.shift = t.single ? 0 : (unsigned char)shift;
     const long long w = t.single ? 1 : GC_CHUNK;
-    t.chunks = (t.pitched ? d.rows : 1) * ((t.n + w - 1) / w);
-    t.whole = t.pitched || t.single ? 0 : t.n / GC_CHUNK / GC_TILE;
+    t.chunks = (t.pitched ? d.rows : 1) * ((t.n + t.shift + w - 1) / w);
+    t.whole = t.pitched || t.single ? 0 : (t.n + t.shift) / GC_CHUNK / GC_TILE;
     t.tile_start = (int)tiles;
     tiles += (t.chunks + GC_TILE - 1) / GC_TILE;
   }

@@ -121,6 +121,29 @@ def test_tensors_off_the_16_byte_boundaries(dtype, shift):
     assert torch.equal(buf.cpu()[outside], keep.cpu()[outside])
 
 
+@pytest.mark.parametrize("dtype,out_dtype", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16),
+                                             (torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)])
+@pytest.mark.parametrize("shift,out_shift", [(1, 1), (3, 3), (0, 1), (2, 0), (5, 5), (3, 7), (1, 5)])
+@pytest.mark.parametrize("rows,cols,pitch", [(1, 40000, 40000), (1, 5, 5), (50, 500, 504), (2, 9000, 9008), (30, 3, 8)])
+def test_tensors_that_begin_anywhere(dtype, out_dtype, shift, out_shift, rows, cols, pitch):
+    """G and out begin elsewhere between two 16-byte boundaries, alike or not; what lies around them stays."""
+    gen = torch.Generator().manual_seed(rows)
+    buf = torch.full((shift + rows * pitch + 16,), float("nan"), dtype=dtype, device="cuda")
+    into = torch.full((out_shift + rows * pitch + 16,), 4.0, dtype=out_dtype, device="cuda")
+    G = buf[shift:shift + rows * pitch].view(rows, pitch)[:, :cols]
+    out = into[out_shift:out_shift + rows * pitch].view(rows, pitch)[:, :cols]
+    G.copy_(torch.randn(rows, cols, generator=gen))
+    was = G.clone()
+    check([was], [out], *fb.clip_grads([G], 1.0, out=[out]), 1.0)
+    outside = torch.ones_like(into, dtype=torch.bool)
+    outside[out_shift:out_shift + rows * pitch].view(rows, pitch)[:, :cols] = False
+    assert bool((into[outside] == 4.0).all()) and torch.equal(G, was)
+    check([was], [G], *fb.clip_grads([G], 1.0), 1.0)
+    outside = torch.ones_like(buf, dtype=torch.bool)
+    outside[shift:shift + rows * pitch].view(rows, pitch)[:, :cols] = False
+    assert bool(buf[outside].isnan().all())
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("size", [1e-38, 1e-30, 1e-22, 1e-19, 1e15, 1e19, 1e25, 1e36])
 def test_the_range_of_the_types(dtype, size):
