@@ -191,11 +191,10 @@ __device__ __forceinline__ unsigned row_fronts(unsigned* counts, int warps, int 
     const unsigned inclusive = warp_inclusive(count);
     if (lane == 31) sum_s[warp] = inclusive;
     __syncthreads();
-    unsigned at = front + inclusive - count;
-    for (int w = 0; w < warps; ++w) {
-      if (w < warp) at += sum_s[w];
-      front += sum_s[w];
-    }
+    const unsigned sums = warp_inclusive(lane < warps ? sum_s[lane] : 0u);
+    const unsigned in_front = __shfl_sync(0xffffffffu, sums, max(warp - 1, 0));
+    const unsigned at = front + (warp ? in_front : 0u) + inclusive - count;
+    front += __shfl_sync(0xffffffffu, sums, 31);
     if (r < nrows) {
       const long long v = ((long long)r << shift) + me;
       if (v < vocab) span[v] = make_int2((int)at, (int)(at + count));
@@ -258,8 +257,7 @@ k_token_order(const TOK* __restrict__ tokens, int n, int vocab, int shift, int n
   below = __reduce_add_sync(0xffffffffu, below);
   if (lane == 0) below_s[warp] = below;
   __syncthreads();
-  unsigned front = 0;
-  for (int w = 0; w < warps; ++w) front += below_s[w];
+  const unsigned front = __reduce_add_sync(0xffffffffu, lane < warps ? below_s[lane] : 0u);
   const unsigned end = row_fronts(shared, warps, nrows, front, shift, me, vocab, span, sum_s);
   if (me == mask && threadIdx.x == 0) *total = (int)end;
   if (listed <= ORD_LIST) {
@@ -319,9 +317,9 @@ k_token_split(const TOK* __restrict__ tokens, int n, int vocab, int blocks, int2
   const unsigned inclusive = warp_inclusive(count);
   if (lane == 31) sum_s[warp] = inclusive;
   __syncthreads();
+  const unsigned in_front = __shfl_sync(0xffffffffu, warp_inclusive(sum_s[lane]), max(warp - 1, 0));
   if (h < blocks) {
-    unsigned at = inclusive - count;
-    for (int w = 0; w < warp; ++w) at += sum_s[w];
+    const unsigned at = (warp ? in_front : 0u) + inclusive - count;
     counts[(long long)h * tiles + tile] = (int)count;
     fronts[(long long)h * tiles + tile] = (int)at;
 #pragma unroll 8
@@ -375,8 +373,7 @@ k_token_gather(const int2* entries, const int* counts, const int* fronts, int ti
     }
   });
   __syncthreads();
-  unsigned front = 0;
-  for (int w = 0; w < warps; ++w) front += below_s[w];
+  const unsigned front = __reduce_add_sync(0xffffffffu, lane < warps ? below_s[lane] : 0u);
   const unsigned end = row_fronts(shared, warps, nrows, front, shift, me, vocab, span, sum_s);
   if (me == gridDim.x - 1 && threadIdx.x == 0) *total = (int)end;
   each([&](bool in, int k, int at) {
