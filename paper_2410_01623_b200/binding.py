@@ -243,12 +243,11 @@ def _grad_words(i: int, g: torch.Tensor, o: torch.Tensor):
 
 
 def _grad_codes(tensors: Sequence[torch.Tensor]):
+    """The type codes of a list: a number where all are of one type, else an array."""
     types = {t.dtype for t in tensors}
     if not types <= _CODES.keys():
         raise ValueError(f"gradients and their outputs are float32 or bfloat16, not {types}")
-    if len(types) == 1:
-        return array("i", (_CODES[types.pop()],)) * len(tensors)
-    return array("i", [_CODES[t.dtype] for t in tensors])
+    return _CODES[types.pop()] if len(types) == 1 else array("i", [_CODES[t.dtype] for t in tensors])
 
 
 def _grad_list(Gs: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]]):
@@ -257,7 +256,6 @@ def _grad_list(Gs: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]]
     n = len(Gs)
     if n == 0:
         raise ValueError("an empty list of gradients")
-    outs = Gs if out is None else out
     codes = _grad_codes(Gs)
     out_codes = codes if out is None else _grad_codes(out)
     devices = set(map(_T.get_device, Gs))
@@ -271,12 +269,16 @@ def _grad_list(Gs: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]]
         words[0::5] = array("q", (1,)) * n
         words[1::5] = array("q", map(_T.numel, Gs))
     else:
-        flat = [w for i, (g, o) in enumerate(zip(Gs, outs)) for w in _grad_words(i, g, o)]
+        flat = [w for i, (g, o) in enumerate(zip(Gs, Gs if out is None else out)) for w in _grad_words(i, g, o)]
         for k in range(4):
             words[k::5] = array("q", flat[k::4])
-    both = array("i", bytes(8 * n))
-    both[0::2], both[1::2] = codes, out_codes
-    words[4::5] = array("q", both.tobytes())
+    if type(codes) is int and type(out_codes) is int:
+        words[4::5] = array("q", (codes | out_codes << 32,)) * n
+    else:
+        both = array("i", bytes(8 * n))
+        both[0::2] = array("i", (codes,)) * n if type(codes) is int else codes
+        both[1::2] = array("i", (out_codes,)) * n if type(out_codes) is int else out_codes
+        words[4::5] = array("q", both.tobytes())
     index = devices.pop()
     if index < 0:
         raise ValueError(f"the Fira library runs on a CUDA device only, not on {Gs[0].device}")
@@ -295,12 +297,12 @@ def grad_norm(Gs: Sequence[torch.Tensor], work: Optional[torch.Tensor] = None) -
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):
             return grad_norm(Gs, work)
-    L, n, device = lib(), len(Gs), Gs[0].device
-    if work is None:
-        work = torch.empty(L.fira_grad_work_bytes(n), dtype=torch.uint8, device=device)
+    L, n = lib(), len(Gs)
+    norm = Gs[0].new_empty((), dtype=torch.float32)
+    if work is None:                           # (float32 by norm's type: the shortest way)
+        work = norm.new_empty(L.fira_grad_work_bytes(n) // 4)
     elif work.get_device() != index:
-        raise ValueError(f"work is on {work.device}, the gradients on {device}")
-    norm = torch.empty((), dtype=torch.float32, device=device)
+        raise ValueError(f"work is on {work.device}, the gradients on {norm.device}")
     status = L.fira_grad_norm(n, words.buffer_info()[0], at.buffer_info()[0], norm.data_ptr(), work.data_ptr(),
                               work.nbytes, _raw_stream(index))
     if status:
@@ -319,12 +321,12 @@ def clip_grads(Gs: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequen
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):
             return clip_grads(Gs, max_norm, out, work)
-    L, n, device = lib(), len(Gs), Gs[0].device
-    if work is None:
-        work = torch.empty(L.fira_grad_work_bytes(n), dtype=torch.uint8, device=device)
+    L, n = lib(), len(Gs)
+    norm = Gs[0].new_empty((), dtype=torch.float32)
+    if work is None:                           # (float32 by norm's type: the shortest way)
+        work = norm.new_empty(L.fira_grad_work_bytes(n) // 4)
     elif work.get_device() != index:
-        raise ValueError(f"work is on {work.device}, the gradients on {device}")
-    norm = torch.empty((), dtype=torch.float32, device=device)
+        raise ValueError(f"work is on {work.device}, the gradients on {norm.device}")
     scale = torch.empty_like(norm)
     status = L.fira_clip_grads(n, words.buffer_info()[0], at.buffer_info()[0],
                                None if out_at is None else out_at.buffer_info()[0], max_norm, norm.data_ptr(),
@@ -339,15 +341,16 @@ def embedding(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0,
     """fira_embedding: scale * table[tokens] (shape of tokens + (hidden,)); zeros where a token is not in 0 .. vocab-1."""
     code = _code(table, "table")
     bits = _TOKEN_BITS.get(tokens.dtype) or _refuse(f"tokens are int32 or int64, not {tokens.dtype}")
-    if table.dim() != 2 or table.numel() == 0:
+    if table.ndim != 2 or table.numel() == 0:
         raise ValueError(f"the table is a matrix, not {tuple(table.shape)}")
     vocab, hidden = table.shape
-    ld = _pitch(table, "table")
+    ld = 0 if table.is_contiguous() else _pitch(table, "table")
     index = _device_of(table, tokens, out)
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):
             return embedding(table, tokens, scale, out)
-    tokens = tokens.contiguous()
+    if not tokens.is_contiguous():
+        tokens = tokens.contiguous()
     if out is None:
         out, ld_out = table.new_empty((*tokens.shape, hidden)), 0
     elif out.shape != (*tokens.shape, hidden) or out.dtype != table.dtype:
@@ -396,10 +399,10 @@ def embedding_grad(tokens: torch.Tensor, dY: torch.Tensor, vocab: int, scale: fl
 
 def _check_params(hidden: int, gain: torch.Tensor, bias: Optional[torch.Tensor], what: str) -> int:
     code = _code(gain, what)
-    for p in (gain, bias):
-        if p is not None and (p.dim() != 1 or p.numel() != hidden or not p.is_contiguous() or p.dtype != gain.dtype):
-            raise ValueError(f"{what}: contiguous vectors of {hidden} elements of one type are needed, not {tuple(p.shape)} "
-                             f"of {p.dtype}")
+    if (gain.ndim != 1 or gain.numel() != hidden or not gain.is_contiguous() or
+            (bias is not None and (bias.ndim != 1 or bias.numel() != hidden or not bias.is_contiguous() or bias.dtype != gain.dtype))):
+        raise ValueError(f"{what}: contiguous vectors of {hidden} elements of one type are needed, not {tuple(gain.shape)} of {gain.dtype}"
+                         + ("" if bias is None else f" and {tuple(bias.shape)} of {bias.dtype}"))
     return code
 
 
@@ -411,10 +414,10 @@ def _check_stats(rows: int, mean: Optional[torch.Tensor], rstd: torch.Tensor, rm
             raise ValueError(f"mean and rstd: {rows} contiguous float32 numbers are needed")
 
 
-def _like(x: torch.Tensor, out: Optional[torch.Tensor]):
-    """A tensor for a result like x, given or new, and its pitch."""
+def _like(x: torch.Tensor, ld: int, out: Optional[torch.Tensor]):
+    """A tensor for a result like x (whose rows are ld apart, 0: contiguous), given or new, and its pitch."""
     if out is None:
-        return (torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)), 0
+        return (x.new_empty(x.shape) if ld else torch.empty_like(x)), 0
     if out.shape != x.shape or out.dtype != x.dtype:
         raise ValueError(f"out: {tuple(x.shape)} of {x.dtype} is needed, not {tuple(out.shape)} of {out.dtype}")
     return out, _pitch(out, "out")
@@ -430,19 +433,20 @@ def layer_norm(x: torch.Tensor, gain: torch.Tensor, bias: Optional[torch.Tensor]
     """fira_layer_norm over the last dimension: (y, mean, rstd); rms: the form without mean and bias (mean is None).  mean
     and rstd are float32 of x's other dimensions, for layer_norm_grad.  out: may be x itself."""
     code = _code(x, "x")
-    if x.dim() == 0 or x.shape[-1] == 0:
-        raise ValueError(f"x has no rows: {tuple(x.shape)}")
-    shape, hidden = x.shape[:-1], x.shape[-1]
+    shape = x.shape
+    hidden = shape[-1] if shape else 0
+    if hidden == 0:
+        raise ValueError(f"x has no rows: {tuple(shape)}")
     params = _check_params(hidden, gain, bias, "gain and bias")
-    ld = _pitch(x, "x")
+    ld = 0 if x.is_contiguous() else _pitch(x, "x")
     index = _device_of(x, gain, bias, out)
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):
             return layer_norm(x, gain, bias, eps, rms, out)
-    out, ld_out = _like(x, out)
-    rstd = x.new_empty(shape, dtype=torch.float32)
+    out, ld_out = _like(x, ld, out)
+    rstd = x.new_empty(shape[:-1], dtype=torch.float32)
     mean = None if rms else torch.empty_like(rstd)
-    status = lib().fira_layer_norm(x.data_ptr(), ld, code, rstd.numel(), hidden, gain.data_ptr(),
+    status = lib().fira_layer_norm(x.data_ptr(), ld, code, x.numel() // hidden, hidden, gain.data_ptr(),
                                    None if bias is None else bias.data_ptr(), params, eps, out.data_ptr(), ld_out,
                                    None if rms else _address(mean), _address(rstd), _raw_stream(index))
     if status:
@@ -458,9 +462,10 @@ def layer_norm_grad(dY: torch.Tensor, x: torch.Tensor, gain: torch.Tensor, mean:
     the gain's type; accumulate: added to what is in them.  work: a byte tensor of at least
     lib().fira_layer_norm_grad_work_bytes() bytes; by default torch's allocator lends one for the call."""
     code = _code(x, "x")
-    if x.dim() == 0 or x.shape[-1] == 0 or dY.shape != x.shape or dY.dtype != x.dtype:
-        raise ValueError(f"dY {tuple(dY.shape)} of {dY.dtype} for x {tuple(x.shape)} of {x.dtype}")
-    hidden = x.shape[-1]
+    shape = x.shape
+    hidden = shape[-1] if shape else 0
+    if hidden == 0 or dY.shape != shape or dY.dtype != x.dtype:
+        raise ValueError(f"dY {tuple(dY.shape)} of {dY.dtype} for x {tuple(shape)} of {x.dtype}")
     rows = x.numel() // hidden
     params = _check_params(hidden, gain, None, "gain")
     _check_stats(rows, mean, rstd, rms)
@@ -468,25 +473,26 @@ def layer_norm_grad(dY: torch.Tensor, x: torch.Tensor, gain: torch.Tensor, mean:
         raise ValueError("the form without mean has no bias")
     if accumulate and (dgain is None or (dbias is None and not rms)):
         raise ValueError("accumulate: dgain and dbias are needed")
-    ld = _pitch(x, "x")
+    ld = 0 if x.is_contiguous() else _pitch(x, "x")
     index = _device_of(x, dY, gain, mean, rstd, out, dgain, dbias, work)
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):
             return layer_norm_grad(dY, x, gain, mean, rstd, rms, out, dgain, dbias, accumulate, work)
     L = lib()
     # a result over dY keeps its place, whatever becomes of dY's rows
-    (out, ld_out), dY = _like(x, out), _rows_or_copy(dY)
+    (out, ld_out), dY = _like(x, ld, out), _rows_or_copy(dY)
+    given = dgain is not None or dbias is not None
     if dgain is None:
         dgain = torch.empty_like(gain)
     if dbias is None and not rms:
         dbias = torch.empty_like(dgain)
-    grads = _check_params(hidden, dgain, dbias, "dgain and dbias")
-    if work is None:
-        work = torch.empty(L.fira_layer_norm_grad_work_bytes(rows, hidden, code) or 1, dtype=torch.uint8, device=x.device)
-    status = L.fira_layer_norm_grad(dY.data_ptr(), _pitch(dY, "dY"), x.data_ptr(), ld, code, rows, hidden, gain.data_ptr(),
-                                    params, None if rms else _address(mean), rstd.data_ptr(), out.data_ptr(), ld_out,
-                                    dgain.data_ptr(), None if rms else dbias.data_ptr(), grads, 1 if accumulate else 0,
-                                    work.data_ptr(), work.nbytes, _raw_stream(index))
+    grads = _check_params(hidden, dgain, dbias, "dgain and dbias") if given else params
+    if work is None:                           # (float32 by rstd's type: the shortest way)
+        work = rstd.new_empty(-(-L.fira_layer_norm_grad_work_bytes(rows, hidden, code) // 4))
+    status = L.fira_layer_norm_grad(dY.data_ptr(), 0 if dY.is_contiguous() else _pitch(dY, "dY"), x.data_ptr(), ld, code, rows,
+                                    hidden, gain.data_ptr(), params, None if rms else _address(mean), rstd.data_ptr(),
+                                    out.data_ptr(), ld_out, dgain.data_ptr(), None if rms else dbias.data_ptr(), grads,
+                                    1 if accumulate else 0, work.data_ptr(), work.nbytes, _raw_stream(index))
     if status:
         check(status)
     return out, dgain, dbias
