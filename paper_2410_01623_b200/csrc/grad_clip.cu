@@ -57,6 +57,23 @@ struct GradTable {
   int count, tiles;
 };
 
+// The tensor of a tile: the last one (q, most often) or found by halving.  (One by one, lists of hundreds of small
+// tensors took 28 us for the norm alone: each look at the table is a miss of the constant cache.)
+__device__ __forceinline__ int find_tensor(const GradEntry* t, int count, int q, int tile) {
+  int lo = 0, hi = count;                   // t[lo].tile_start <= tile, and t[hi]'s is not
+  if (tile >= t[q].tile_start) {
+    if (q + 1 == count || tile < t[q + 1].tile_start) return q;
+    lo = q + 1;
+  } else {
+    hi = q;
+  }
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (t[mid].tile_start <= tile) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
 // Where chunk c of the tensor starts in G and in out, and how many elements it has.
 struct Place { long long at, out_at; int len; };
 __device__ __forceinline__ Place place(const GradEntry& t, long long c, long long row0, unsigned col0, unsigned local) {
@@ -252,7 +269,7 @@ k_grad_squares(const __grid_constant__ GradTable<CAP> tab, double* __restrict__ 
   double total = 0.0;
   int q = 0;
   for (int tile = blockIdx.x; tile < tab.tiles; tile += gridDim.x) {
-    while (q + 1 < tab.count && tile >= tab.t[q + 1].tile_start) ++q;
+    q = find_tensor(tab.t, tab.count, q, tile);
     const GradEntry& t = tab.t[q];
     if (is_whole(t, tile)) {
       const uint64_t pol = tile >= kept ? again : once;
@@ -299,7 +316,7 @@ k_grad_scale(const __grid_constant__ GradTable<CAP> tab, const double* sums, int
   int q = tab.count - 1;
   // from the end: what the sums read last is what the L2 still holds
   for (int tile = tab.tiles - 1 - (int)blockIdx.x; tile >= 0; tile -= gridDim.x) {
-    while (tile < tab.t[q].tile_start) --q;
+    q = find_tensor(tab.t, tab.count, q, tile);
     const GradEntry& t = tab.t[q];
     if (is_whole(t, tile)) {
       const long long first = (long long)(tile - t.tile_start) * GC_TILE;
