@@ -4,7 +4,7 @@
 //   with h = (x - mu) s, q = dy g:   dx = s (q - mean(q) - h mean(q h))   (RMS: without mean(q))
 //   dg = sum over rows of dy h,   db = sum over rows of dy
 //
-// A group of 32 to 1024 threads takes a row, each thread 16 elements of it, which stay in registers (as they were read)
+// A group of 4 to 1024 threads takes a row, each thread 16 elements of it, which stay in registers (as they were read)
 // from the load to the store; the next row is on its way meanwhile.  Gain and bias lie in shared memory in the order in which
 // the threads read them.  Statistics are fp32, the variance from the differences to the mean.  In the backward pass a
 // thread has the same columns in every row of its group, so that dg and db grow in its registers; the groups of a block are added in shared memory, the
@@ -30,7 +30,9 @@ constexpr int LN_SMS = 148;
 // The threads of a row, and this thread's place.
 struct Group {
   int threads, id, rank, count;             // id of count groups in the block
-  __device__ __forceinline__ explicit Group(int per_row) : threads(per_row), id(threadIdx.x / per_row), rank(threadIdx.x % per_row), count(blockDim.x / per_row) {}
+  unsigned mask;                            // its lanes, where it is a part of a warp
+  __device__ __forceinline__ explicit Group(int per_row) : threads(per_row), id(threadIdx.x / per_row), rank(threadIdx.x % per_row), count(blockDim.x / per_row),
+    mask(per_row >= 32 ? 0xffffffffu : ((1u << per_row) - 1) << (threadIdx.x & 31 & ~(per_row - 1))) {}
 };
 
 // (LN_THREADS is four groups of two warps at most.)
@@ -47,10 +49,11 @@ template <int VALUES>
 __device__ __forceinline__ float2 group_sum(float2 v, const Group& g, float2 (*red)[32], int& turn) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
-    v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-    if (VALUES == 2) v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+    if (o >= g.threads) continue;           // (a part of a warp: the others may be elsewhere)
+    v.x += __shfl_xor_sync(g.mask, v.x, o);
+    if (VALUES == 2) v.y += __shfl_xor_sync(g.mask, v.y, o);
   }
-  if (g.threads == 32) return v;
+  if (g.threads <= 32) return v;
   const int lane = threadIdx.x & 31, warps = g.threads >> 5, first = g.id * warps;
   if (lane == 0) red[turn][threadIdx.x >> 5] = v;
   group_barrier(g);
@@ -162,15 +165,15 @@ template <typename T, bool BIG, bool RMS>
 constexpr int NORM_STAGES = !BIG && RMS && sizeof(T) == 2 ? 3 : !BIG || RMS || sizeof(T) == 2 ? 2 : 1;
 template <typename T, bool BIG, bool RMS>
 constexpr size_t NORM_SMEM = (RMS ? 1 : 2) * LN_EACH * sizeof(float) + NORM_STAGES<T, BIG, RMS> * LN_EACH * sizeof(T);     // per thread
-template <typename T, bool BIG>
-constexpr int GRAD_STAGES = BIG ? (sizeof(T) == 2 ? 2 : 1) : (sizeof(T) == 2 ? 3 : 2);
-template <typename T, bool BIG>
-constexpr size_t GRAD_SMEM = (size_t)LN_EACH * sizeof(float) + 2 * GRAD_STAGES<T, BIG> * LN_EACH * sizeof(T);
+template <typename T, int THREADS>
+constexpr int GRAD_STAGES = THREADS == 1024 ? (sizeof(T) == 2 ? 2 : 1) : THREADS == 512 ? (sizeof(T) == 2 ? 4 : 2) : (sizeof(T) == 2 ? 3 : 2);
+template <typename T, int THREADS>
+constexpr size_t GRAD_SMEM = (size_t)LN_EACH * sizeof(float) + 2 * GRAD_STAGES<T, THREADS> * LN_EACH * sizeof(T);
 
-// Blocks of the backward pass on an SM (where rows take LN_THREADS threads at most): the registers of both gradients' sums
-// leave room for two.
-template <bool RMS>
-constexpr int GRAD_RESIDENT = RMS ? 3 : 2;
+// Blocks of the backward pass on an SM (where rows take LN_THREADS threads at most): three where the registers suffice (65536 rows of
+// 512, bf16, without mean: 45 us), two of more registers elsewhere (of 256, fp32: 62 us with three, 43 with two).
+template <typename T, Mode MODE, bool RMS, int THREADS>
+constexpr int GRAD_RESIDENT = THREADS > LN_THREADS ? 1 : RMS && MODE == ALIGNED && sizeof(T) == 2 ? 3 : 2;
 
 // BIG: rows of more than LN_THREADS threads.
 template <typename T, Mode MODE, bool BIG, bool RMS>
@@ -262,15 +265,15 @@ k_layer_norm(const T* x, long long ld_x, long long nrows, int hidden, int per_ro
 }
 
 // parts: per block the sums of dy h, then (want_bias) those of dy, `hidden` floats each.
-template <typename T, Mode MODE, bool BIG, bool RMS>
-__global__ void __launch_bounds__(BIG ? 1024 : LN_THREADS, BIG ? 1 : GRAD_RESIDENT<RMS>)
+template <typename T, Mode MODE, int THREADS, bool RMS>
+__global__ void __launch_bounds__(THREADS, (GRAD_RESIDENT<T, MODE, RMS, THREADS>))
 k_layer_norm_grad(const T* dy, long long ld_dy, const T* x, long long ld_x, long long nrows, int hidden, int per_row, const void* gain,
                   int param_bf16, const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, long long ld_dx,
                   float* __restrict__ parts, int want_bias) {
   using C = Cols<T, MODE>;
-  constexpr int N = C::N, PIECES = C::PIECES, STAGES = GRAD_STAGES<T, BIG>;
-  constexpr bool KEEP = RMS && !BIG;        // h and q stay in registers while the sums are made: where there are registers
-  static_assert((BIG ? 1024 : LN_THREADS) * GRAD_SMEM<T, BIG> + 2048 <= 227 * 1024, "shared memory of a block");
+  constexpr int N = C::N, PIECES = C::PIECES, STAGES = GRAD_STAGES<T, THREADS>;
+  constexpr bool KEEP = RMS && THREADS < 1024;        // h and q stay in registers while the sums are made: where there are registers
+  static_assert(THREADS * GRAD_SMEM<T, THREADS> + 2048 <= 227 * 1024, "shared memory of a block");
   extern __shared__ float4 kept4[];         // gains of every group; then sums of the groups; behind them the rows on their way
   __shared__ float2 red[2][32];
   ptx::grid_launch_next();
@@ -340,6 +343,7 @@ k_layer_norm_grad(const T* dy, long long ld_dy, const T* x, long long ld_x, long
           dg[p][e] = rows::fma2(d[e], h[p][e], dg[p][e]);
           if (!RMS) { level2 = rows::add2(level2, q[p][e]); db[p][e] = rows::add2(db[p][e], d[e]); }
         }
+        if (!KEEP) asm volatile("" ::: "memory");     // one piece after the other: registers
       }
       const float2 s = group_sum<RMS ? 1 : 2>(make_float2(along2.x + along2.y, level2.x + level2.y), g, red, turn);
       const float2 along = rows::both(-s.x * inv), level = rows::both(-s.y * inv);
@@ -350,6 +354,7 @@ k_layer_norm_grad(const T* dy, long long ld_dy, const T* x, long long ld_x, long
         for (int e = 0; e < N / 2; ++e)
           h[p][e] = rows::mul2(rows::both(rs), rows::fma2(h[p][e], along, RMS ? q[p][e] : rows::add2(q[p][e], level)));
         cols.store(dx + row * ld_dx, p, h[p]);
+        if (!KEEP) asm volatile("" ::: "memory");
       }
       if (!more) break;
       row += stride;
@@ -357,13 +362,30 @@ k_layer_norm_grad(const T* dy, long long ld_dy, const T* x, long long ld_x, long
       stage = stage + 1 == STAGES ? 0 : stage + 1;
     }
   }
-  // the groups one after another
+  // Groups of a warp that have the same columns by shuffles, then the groups (or warps) one after another.
+  int turns = g.count, turn = g.id;
+  if (MODE != SHIFTED && g.threads < 32) {
+    __syncwarp();
+#pragma unroll
+    for (int o = 4; o < 32; o *= 2) {
+      if (o < g.threads) continue;
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e) {
+          dg[p][e].x += __shfl_xor_sync(0xffffffffu, dg[p][e].x, o); dg[p][e].y += __shfl_xor_sync(0xffffffffu, dg[p][e].y, o);
+          if (!RMS) { db[p][e].x += __shfl_xor_sync(0xffffffffu, db[p][e].x, o); db[p][e].y += __shfl_xor_sync(0xffffffffu, db[p][e].y, o); }
+        }
+    }
+    turns = blockDim.x / 32;
+    turn = (threadIdx.x & 31) < g.threads ? (int)(threadIdx.x / 32) : -1;
+  }
   float* sums = reinterpret_cast<float*>(kept4);      // [2 or 1][hidden]: where there are groups, no more than the gains took
-  if (g.count > 1) __syncthreads();
+  if (turns > 1) __syncthreads();
   float* out = parts + (long long)blockIdx.x * hidden * (want_bias ? 2 : 1);
-  for (int k = 0; k < g.count; ++k) {
-    if (g.id == k) {
-      float* to = k + 1 < g.count ? sums : out;
+  for (int k = 0; k < turns; ++k) {
+    if (turn == k) {
+      float* to = k + 1 < turns ? sums : out;
 #pragma unroll
       for (int p = 0; p < PIECES; ++p)
 #pragma unroll
@@ -378,7 +400,7 @@ k_layer_norm_grad(const T* dy, long long ld_dy, const T* x, long long ld_x, long
           }
         }
     }
-    if (g.count > 1) __syncthreads();
+    if (turns > 1) __syncthreads();
   }
 }
 
@@ -424,7 +446,7 @@ RowPlan rows_of(long long hidden, size_t size, Mode mode) {
   const long long extent = hidden + (mode == SHIFTED ? 16 / (long long)size - 1 : 0);
   if (extent > LN_MAX_HIDDEN) return rows_of(hidden, size, SINGLE);
   p.mode = mode;
-  p.per_row = 32;
+  p.per_row = 4;
   while ((long long)p.per_row * LN_EACH < extent) p.per_row *= 2;
   p.threads = std::max(LN_THREADS, p.per_row);
   p.groups = p.threads / p.per_row;
@@ -440,8 +462,9 @@ long long blocks_for(const RowPlan& p, long long nrows, long long most, long lon
 }
 // Blocks of the backward pass: as many as are resident at once, and four rows at least for a group, since each block
 // writes its sums of dg and db.
-int grad_blocks(const RowPlan& p, long long nrows, bool rms) {
-  return (int)blocks_for(p, nrows, (p.big ? 1 : rms ? GRAD_RESIDENT<true> : GRAD_RESIDENT<false>) * LN_SMS / 8 * 8, 4);
+int grad_blocks(const RowPlan& p, long long nrows, bool rms, size_t size) {
+  const int resident = p.big ? 1 : rms && p.mode == ALIGNED && size == 2 ? GRAD_RESIDENT<__nv_bfloat16, ALIGNED, true, LN_THREADS> : GRAD_RESIDENT<float, SINGLE, false, LN_THREADS>;
+  return (int)blocks_for(p, nrows, resident * LN_SMS / 8 * 8, 4);
 }
 
 template <typename T, Mode MODE, bool BIG, bool RMS>
@@ -457,15 +480,19 @@ cudaError_t run_forward(const RowPlan& p, const void* x, long long ld_x, long lo
   k_layer_norm<T, MODE, BIG, RMS><<<blocks, p.threads, smem, st>>>((const T*)x, ld_x, nrows, hidden, p.per_row, gain, bias, param_bf16, eps, (T*)y, ld_y, mean, rstd);
   return cudaGetLastError();
 }
-template <typename T, Mode MODE, bool BIG, bool RMS>
-cudaError_t run_backward(const RowPlan& p, const void* dy, long long ld_dy, const void* x, long long ld_x, long long nrows, int hidden, const void* gain,
-                         int param_bf16, const float* mean, const float* rstd, void* dx, long long ld_dx, float* parts, int want_bias, cudaStream_t st) {
-  const size_t smem = p.threads * GRAD_SMEM<T, BIG>;
-  const cudaError_t e = cudaFuncSetAttribute(k_layer_norm_grad<T, MODE, BIG, RMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)((BIG ? 1024 : LN_THREADS) * GRAD_SMEM<T, BIG>));
+template <typename T, Mode MODE, int THREADS, bool RMS>
+cudaError_t run_backward_of(const RowPlan& p, const void* dy, long long ld_dy, const void* x, long long ld_x, long long nrows, int hidden, const void* gain,
+                            int param_bf16, const float* mean, const float* rstd, void* dx, long long ld_dx, float* parts, int want_bias, cudaStream_t st) {
+  const cudaError_t e = cudaFuncSetAttribute(k_layer_norm_grad<T, MODE, THREADS, RMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(THREADS * GRAD_SMEM<T, THREADS>));
   if (e != cudaSuccess) return e;
-  k_layer_norm_grad<T, MODE, BIG, RMS><<<grad_blocks(p, nrows, RMS), p.threads, smem, st>>>(
+  k_layer_norm_grad<T, MODE, THREADS, RMS><<<grad_blocks(p, nrows, RMS, sizeof(T)), p.threads, p.threads * GRAD_SMEM<T, THREADS>, st>>>(
       (const T*)dy, ld_dy, (const T*)x, ld_x, nrows, hidden, p.per_row, gain, param_bf16, mean, rstd, (T*)dx, ld_dx, parts, want_bias);
   return cudaGetLastError();
+}
+template <typename T, Mode MODE, bool BIG, bool RMS, typename... A>
+cudaError_t run_backward(const RowPlan& p, A... a) {
+  if constexpr (!BIG) return run_backward_of<T, MODE, LN_THREADS, RMS>(p, a...);
+  else return p.per_row == 512 ? run_backward_of<T, MODE, 512, RMS>(p, a...) : run_backward_of<T, MODE, 1024, RMS>(p, a...);
 }
 
 fira_status check_norm(const std::string& who, int64_t rows, int64_t hidden, fira_dtype dtype, fira_dtype param_dtype) {
@@ -542,7 +569,7 @@ extern "C" size_t fira_layer_norm_grad_work_bytes(int64_t nrows, int64_t hidden,
   const size_t es = dtype == FIRA_BF16 ? 2 : 4;
   int blocks = 0;                           // however the rows will begin
   for (const Mode mode : {SINGLE, SHIFTED, ALIGNED})
-    for (const bool rms : {false, true}) blocks = std::max(blocks, grad_blocks(rows_of(hidden, es, mode), nrows, rms));
+    for (const bool rms : {false, true}) blocks = std::max(blocks, grad_blocks(rows_of(hidden, es, mode), nrows, rms, es));
   return align_up((size_t)blocks * 2 * hidden * sizeof(float));
 }
 
@@ -579,7 +606,7 @@ extern "C" fira_status fira_layer_norm_grad(const void* dY_dev, int64_t ld_dy, c
 #undef LN_BACKWARD
     const int width = (int)hidden * (want_bias ? 2 : 1);
     if (e == cudaSuccess)
-      e = launch_chained(k_layer_norm_params, dim3((width + 31) / 32), 1024, 0, st, true, 1, (const float*)parts, grad_blocks(p, nrows, rms), width,
+      e = launch_chained(k_layer_norm_params, dim3((width + 31) / 32), 1024, 0, st, true, 1, (const float*)parts, grad_blocks(p, nrows, rms, es), width,
                          (int)hidden, dgain_dev, dbias_dev, grad_dtype == FIRA_BF16 ? 1 : 0, accumulate != 0 ? 1 : 0);
     if (e != cudaSuccess) { set_error(who + ": " + cudaGetErrorString(e)); return FIRA_ERR_CUDA; }
     return FIRA_OK;
