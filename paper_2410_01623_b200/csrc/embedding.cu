@@ -28,7 +28,6 @@ constexpr int EM_SMS = 148;
 
 // ------------------------------------------------------------------------------------------------ lookup
 constexpr int LK_ROWS = 4;                 // rows of a warp in flight
-constexpr int LK_EACH = 2;                 // words of a thread
 
 template <typename TOK>
 __device__ __forceinline__ int token_at(const TOK* tokens, long long i, int vocab) {
@@ -64,57 +63,70 @@ k_embedding_rows(const T* __restrict__ table, long long ld, const TOK* __restric
   }
 }
 
-// The output goes by words of 16 aligned bytes, `words` to a row, which are dealt to the threads in a row of their own, so that
-// rows of any width keep all lanes busy; a thread has LK_EACH of them.  ALIGNED: all rows are whole 16-byte units on
-// 16-byte boundaries.  Otherwise a word is funnelled from two aligned words of the table, of which those are read that
-// hold a byte of it.
+// The output goes by items of one or two words of 16 aligned bytes, `items` to a row, which are dealt to the threads in a row of their
+// own, so that rows of any width keep all lanes busy.  ALIGNED (one word, two items of a thread): all rows are whole
+// 16-byte units on 16-byte boundaries.  Otherwise (two words, one item) they are funnelled from three aligned words of the table,
+// of which those are read that hold a byte of them (131072 rows of 1023, bf16: 83 us; one word and two items 103).
+template <bool ALIGNED>
+constexpr int LK_WORDS = ALIGNED ? 1 : 2;
+template <bool ALIGNED>
+constexpr int LK_ITEMS = ALIGNED ? 2 : 1;
+
 template <typename T, typename TOK, bool ALIGNED>
 __global__ void __launch_bounds__(EM_THREADS)
-k_embedding_words(const T* __restrict__ table, long long ld, const TOK* __restrict__ tokens, long long n, int vocab, int hidden, unsigned words,
-            float scale, T* __restrict__ out, long long ld_out) {
-  constexpr int N = rows::PER16<T>;
-  const long long first = (long long)blockIdx.x * (EM_THREADS * LK_EACH), row0 = first / words;
-  const unsigned word0 = (unsigned)(first - row0 * words);
-  uint4 a[LK_EACH], b[LK_EACH];
-  T* to[LK_EACH];                           // the word, and the column of its first element (hidden: none)
+k_embedding_words(const T* __restrict__ table, long long ld, const TOK* __restrict__ tokens, long long n, int vocab, int hidden, unsigned items,
+                  float scale, T* __restrict__ out, long long ld_out) {
+  constexpr int N = rows::PER16<T>, W = LK_WORDS<ALIGNED>, LK_EACH = LK_ITEMS<ALIGNED>;
+  const long long first = (long long)blockIdx.x * (EM_THREADS * LK_EACH), row0 = first / items;
+  const unsigned item0 = (unsigned)(first - row0 * items);
+  uint4 a[LK_EACH][W + (ALIGNED ? 0 : 1)];
+  T* to[LK_EACH];                           // the first word, and the column of its first element (hidden: none)
   int col[LK_EACH], skip[LK_EACH];
 #pragma unroll
   for (int u = 0; u < LK_EACH; ++u) {
-    const unsigned x = word0 + u * EM_THREADS + threadIdx.x, down = x / words;      // (words < 2^23: no overflow)
+    const unsigned x = item0 + u * EM_THREADS + threadIdx.x, down = x / items;      // (items < 2^23: no overflow)
     const long long i = row0 + down;
-    a[u] = b[u] = make_uint4(0u, 0u, 0u, 0u);
-    col[u] = hidden; skip[u] = 0;
+#pragma unroll
+    for (int w = 0; w < W + (ALIGNED ? 0 : 1); ++w) a[u][w] = make_uint4(0u, 0u, 0u, 0u);
+    col[u] = hidden; skip[u] = 0; to[u] = out;
     if (i >= n) continue;
     const int t = token_at(tokens, i, vocab);
     T* out_row = out + i * ld_out;
     const T* row = table + (long long)max(t, 0) * ld;
-    col[u] = (int)(x - down * words) * N;
+    col[u] = (int)(x - down * items) * (N * W);
     if (ALIGNED) {
-      if (t >= 0) a[u] = *reinterpret_cast<const uint4*>(row + col[u]);
+      if (t >= 0) a[u][0] = *reinterpret_cast<const uint4*>(row + col[u]);
     } else {
       col[u] -= (int)(((uintptr_t)out_row & 15) / sizeof(T));
-      const uintptr_t from = (uintptr_t)(row + max(col[u], 0)), end = (uintptr_t)(row + min(col[u] + N, hidden));     // the bytes that are wanted
+      const uintptr_t from = (uintptr_t)(row + max(col[u], 0)), end = (uintptr_t)(row + min(col[u] + N * W, hidden));     // the bytes that are wanted
       const uintptr_t begin = (uintptr_t)(row + col[u]), word = begin & ~(uintptr_t)15;
       skip[u] = (int)(begin & 15);
       if (t >= 0 && from < end) {
-        if (word + 16 > from) a[u] = *reinterpret_cast<const uint4*>(word);
-        if (word + 16 < end) b[u] = *reinterpret_cast<const uint4*>(word + 16);
+#pragma unroll
+        for (int w = 0; w < W + 1; ++w)
+          if (word + 16 * w + 16 > from && word + 16 * w < end) a[u][w] = *reinterpret_cast<const uint4*>(word + 16 * w);
       }
     }
     to[u] = out_row + col[u];
   }
 #pragma unroll
   for (int u = 0; u < LK_EACH; ++u) {
-    if (!ALIGNED) a[u] = rows::funnel16(a[u], b[u], skip[u]);
-    float2 v[N / 2];
-    rows::unpack<T>(a[u], v);
 #pragma unroll
-    for (int e = 0; e < N / 2; ++e) v[e] = rows::mul2(v[e], rows::both(scale));
-    const uint4 w = rows::pack<T>(v);
-    if (ALIGNED) {
-      if (col[u] < hidden) *reinterpret_cast<uint4*>(to[u]) = w;
-    } else {
-      if (col[u] < hidden) rows::store_between(to[u], w, col[u], 0, hidden);
+    for (int w = 0; w < W; ++w) {
+      uint4 x = a[u][w];
+      if constexpr (!ALIGNED) x = rows::funnel16(a[u][w], a[u][w + 1], skip[u]);
+      if (scale != 1.f) {
+        float2 v[N / 2];
+        rows::unpack<T>(x, v);
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e) v[e] = rows::mul2(v[e], rows::both(scale));
+        x = rows::pack<T>(v);
+      }
+      if (ALIGNED) {
+        if (col[u] < hidden) *reinterpret_cast<uint4*>(to[u]) = x;
+      } else {
+        if (col[u] + w * N < hidden) rows::store_between(to[u] + w * N, x, col[u] + w * N, 0, hidden);
+      }
     }
   }
 }
@@ -724,16 +736,17 @@ template <typename T, typename TOK>
 void run_lookup(const void* table, long long ld, const void* tokens, long long n, int vocab, int hidden, float scale, void* out, long long ld_out,
                 cudaStream_t st) {
   const bool aligned = rows::aligned16(table, ld, hidden, sizeof(T)) && rows::aligned16(out, ld_out, hidden, sizeof(T));
-  const unsigned words = words_of(hidden, sizeof(T), aligned);
-  const unsigned blocks = (unsigned)((n * words + EM_THREADS * LK_EACH - 1) / (EM_THREADS * LK_EACH));
+  const unsigned words = words_of(hidden, sizeof(T), aligned), items = aligned ? words : (words + LK_WORDS<false> - 1) / LK_WORDS<false>;
+  const int per_block = EM_THREADS * (aligned ? LK_ITEMS<true> : LK_ITEMS<false>);
+  const unsigned blocks = (unsigned)((n * items + per_block - 1) / per_block);
   if (aligned && words >= 96) {              // (the last slice of 32 leaves a quarter of the lanes idle at most)
     const int slices = (int)((words + 31) / 32);
     k_embedding_rows<T, TOK><<<(unsigned)(((n + LK_ROWS - 1) / LK_ROWS * slices + EM_WARPS - 1) / EM_WARPS), EM_THREADS, 0, st>>>(
         (const T*)table, ld, (const TOK*)tokens, n, vocab, hidden, slices, scale, (T*)out, ld_out);
   } else if (aligned)
-    k_embedding_words<T, TOK, true><<<blocks, EM_THREADS, 0, st>>>((const T*)table, ld, (const TOK*)tokens, n, vocab, hidden, words, scale, (T*)out, ld_out);
+    k_embedding_words<T, TOK, true><<<blocks, EM_THREADS, 0, st>>>((const T*)table, ld, (const TOK*)tokens, n, vocab, hidden, items, scale, (T*)out, ld_out);
   else
-    k_embedding_words<T, TOK, false><<<blocks, EM_THREADS, 0, st>>>((const T*)table, ld, (const TOK*)tokens, n, vocab, hidden, words, scale, (T*)out, ld_out);
+    k_embedding_words<T, TOK, false><<<blocks, EM_THREADS, 0, st>>>((const T*)table, ld, (const TOK*)tokens, n, vocab, hidden, items, scale, (T*)out, ld_out);
 }
 
 // Counts and lists may be above the default limit of shared memory: a setting per device and kernel.
@@ -807,7 +820,7 @@ extern "C" fira_status fira_embedding(const void* table_dev, int64_t vocab, int6
     if (!table_dev || !tokens_dev || !out_dev || (((uintptr_t)table_dev | (uintptr_t)out_dev) & (es - 1)) || ((uintptr_t)tokens_dev & (token_bits / 8 - 1))) {
       set_error("fira_embedding: pointers must be non-null and aligned to their elements"); return FIRA_ERR_INVALID_ARG;
     }
-    if (count * words_of(hidden, es, false) > 0x7fffffffll * EM_THREADS * LK_EACH) { set_error("fira_embedding: too many elements in one call"); return FIRA_ERR_INVALID_ARG; }
+    if (count * words_of(hidden, es, false) > 0x7fffffffll * EM_THREADS) { set_error("fira_embedding: too many elements in one call"); return FIRA_ERR_INVALID_ARG; }
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (dtype == FIRA_BF16) {
       if (token_bits == 32) run_lookup<__nv_bfloat16, int>(table_dev, ld, tokens_dev, count, (int)vocab, (int)hidden, scale, out_dev, ld_out, st);
