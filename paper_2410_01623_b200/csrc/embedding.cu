@@ -225,7 +225,7 @@ template <typename TOK, bool VECTOR>
 __global__ void __launch_bounds__(ORD_MAX_THREADS)
 k_token_order(const TOK* __restrict__ tokens, int n, int vocab, int shift, int nrows, int2* __restrict__ order, int2* __restrict__ span,
               int* __restrict__ total, unsigned* __restrict__ counters, long long ncounters) {
-  extern __shared__ unsigned shared[];      // counts [warps][nrows], lists [warps][ORD_LIST] of (position, row)
+  extern __shared__ __align__(16) unsigned shared[];      // counts [warps][nrows], lists [warps][ORD_LIST] of (position, row)
   __shared__ unsigned below_s[32], sum_s[32];
   ptx::grid_launch_next();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, threads = blockDim.x;
@@ -303,7 +303,7 @@ template <typename TOK>
 __global__ void __launch_bounds__(ORD_TILE)
 k_token_split(const TOK* __restrict__ tokens, int n, int vocab, int blocks, int2* __restrict__ entries, int* __restrict__ counts, int* __restrict__ fronts,
               unsigned* __restrict__ counters, long long ncounters) {
-  extern __shared__ unsigned shared[];      // [32 warps][blocks]
+  extern __shared__ __align__(16) unsigned shared[];      // [32 warps][blocks]
   __shared__ unsigned sum_s[32];
   ptx::grid_launch_next();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tile = blockIdx.x, tiles = gridDim.x;
@@ -344,7 +344,7 @@ k_token_split(const TOK* __restrict__ tokens, int n, int vocab, int blocks, int2
 // Block b sorts the entries of remainder b by row; a warp takes the tiles of a stretch.  Otherwise as k_token_order.
 __global__ void __launch_bounds__(ORD_MAX_THREADS)
 k_token_gather(const int2* entries, const int* counts, const int* fronts, int tiles, int vocab, int shift, int nrows, int2* order, int2* span, int* total) {
-  extern __shared__ unsigned shared[];      // counts [warps][nrows], lists [warps][ORD_LIST] of (position, token)
+  extern __shared__ __align__(16) unsigned shared[];      // counts [warps][nrows], lists [warps][ORD_LIST] of (position, token)
   __shared__ unsigned below_s[32], sum_s[32];
   ptx::grid_launch_next();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, threads = blockDim.x;
