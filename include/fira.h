@@ -219,7 +219,8 @@ FIRA_API fira_status fira_clip_grads(int32_t count, const fira_grad_desc* descs,
  * as zeros.  accumulate != 0: the sums are added to what is there (micro-batches; a table that is also the output head),
  * and rows without a token are left alone.  work_dev: 256-byte aligned, fira_embedding_grad_work_bytes() bytes of the same
  * sizes (0: sizes that the call refuses), of one call at a time; its contents need not be kept or set.
- * count = 0 is allowed.  Need no context.  Asynchronous on cuda_stream. */
+ * count = 0 is allowed.  Rows are read in aligned 16-byte words: the other bytes of a word that holds an element of a row are
+ * read with it, and not used.  Need no context.  Asynchronous on cuda_stream. */
 FIRA_API fira_status fira_embedding(const void* table_dev, int64_t vocab, int64_t hidden, int64_t ld, fira_dtype dtype,
                                     const void* tokens_dev, int32_t token_bits, int64_t count, float scale,
                                     void* out_dev, int64_t ld_out, void* cuda_stream);
@@ -242,8 +243,8 @@ FIRA_API fira_status fira_embedding_grad(const void* tokens_dev, int32_t token_b
  * every call.  accumulate != 0: dgain and dbias are added to what is there.
  * y may be x itself, dX may be dY or x itself (same ld); otherwise they overlap nothing.  nrows = 0 is allowed (dgain and dbias
  * are then zero, or left as they are).  work_dev: 256-byte aligned, fira_layer_norm_grad_work_bytes() bytes of the same
- * sizes (0: sizes that the call refuses), of one call at a time; its contents need not be kept or set.  Need no context.
- * Asynchronous on cuda_stream. */
+ * sizes (0: sizes that the call refuses), of one call at a time; its contents need not be kept or set.  Rows are read in
+ * aligned 16-byte words, as by fira_embedding().  Need no context.  Asynchronous on cuda_stream. */
 FIRA_API fira_status fira_layer_norm(const void* x_dev, int64_t ld_x, fira_dtype dtype, int64_t nrows, int64_t hidden,
                                      const void* gain_dev, const void* bias_dev, fira_dtype param_dtype, float eps,
                                      void* y_dev, int64_t ld_y, float* mean_dev, float* rstd_dev, void* cuda_stream);

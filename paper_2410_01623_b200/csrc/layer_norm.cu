@@ -45,15 +45,16 @@ __device__ __forceinline__ void group_barrier(const Group& g) {
 }
 
 // Sums over the group of one or two values of each thread.  Calls use the two buffers in turn, so that one barrier is enough.
-template <int VALUES>
+// PART: the group is a part of a warp (the others of the warp may be elsewhere).
+template <int VALUES, bool PART>
 __device__ __forceinline__ float2 group_sum(float2 v, const Group& g, float2 (*red)[32], int& turn) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
-    if (o >= g.threads) continue;           // (a part of a warp: the others may be elsewhere)
-    v.x += __shfl_xor_sync(g.mask, v.x, o);
-    if (VALUES == 2) v.y += __shfl_xor_sync(g.mask, v.y, o);
+    if (PART && o >= g.threads) continue;
+    v.x += __shfl_xor_sync(PART ? g.mask : 0xffffffffu, v.x, o);
+    if (VALUES == 2) v.y += __shfl_xor_sync(PART ? g.mask : 0xffffffffu, v.y, o);
   }
-  if (g.threads <= 32) return v;
+  if (PART || g.threads == 32) return v;
   const int lane = threadIdx.x & 31, warps = g.threads >> 5, first = g.id * warps;
   if (lane == 0) red[turn][threadIdx.x >> 5] = v;
   group_barrier(g);
@@ -161,10 +162,10 @@ template <typename T>
 __device__ __forceinline__ int shift_of(const T* row) { return (int)(((uintptr_t)row & 15) / sizeof(T)); }
 
 // Rows on their way to shared memory, the one that is worked on among them: as many as there is room for.
-template <typename T, bool BIG, bool RMS>
-constexpr int NORM_STAGES = !BIG && RMS && sizeof(T) == 2 ? 3 : !BIG || RMS || sizeof(T) == 2 ? 2 : 1;
-template <typename T, bool BIG, bool RMS>
-constexpr size_t NORM_SMEM = (RMS ? 1 : 2) * LN_EACH * sizeof(float) + NORM_STAGES<T, BIG, RMS> * LN_EACH * sizeof(T);     // per thread
+template <typename T, bool LONG, bool RMS>
+constexpr int NORM_STAGES = !LONG && RMS && sizeof(T) == 2 ? 3 : !LONG || RMS || sizeof(T) == 2 ? 2 : 1;
+template <typename T, bool LONG, bool RMS>
+constexpr size_t NORM_SMEM = (RMS ? 1 : 2) * LN_EACH * sizeof(float) + NORM_STAGES<T, LONG, RMS> * LN_EACH * sizeof(T);     // per thread
 template <typename T, int THREADS>
 constexpr int GRAD_STAGES = THREADS == 1024 ? (sizeof(T) == 2 ? 2 : 1) : THREADS == 512 ? (sizeof(T) == 2 ? 4 : 2) : (sizeof(T) == 2 ? 3 : 2);
 template <typename T, int THREADS>
@@ -175,14 +176,16 @@ constexpr size_t GRAD_SMEM = (size_t)LN_EACH * sizeof(float) + 2 * GRAD_STAGES<T
 template <typename T, Mode MODE, bool RMS, int THREADS>
 constexpr int GRAD_RESIDENT = THREADS > LN_THREADS ? 1 : RMS && MODE == ALIGNED && sizeof(T) == 2 ? 3 : 2;
 
-// BIG: rows of more than LN_THREADS threads.
-template <typename T, Mode MODE, bool BIG, bool RMS>
-__global__ void __launch_bounds__(BIG ? 1024 : LN_THREADS, BIG ? 1 : 4)
+// SIZE: rows of a part of a warp, of up to LN_THREADS threads, of more.
+enum Size { PART, SOME, BIG };
+
+template <typename T, Mode MODE, Size SIZE, bool RMS>
+__global__ void __launch_bounds__(SIZE == BIG ? 1024 : LN_THREADS, SIZE == BIG ? 1 : 4)
 k_layer_norm(const T* x, long long ld_x, long long nrows, int hidden, int per_row, const void* gain, const void* bias, int param_bf16, float eps,
              T* y, long long ld_y, float* __restrict__ mean, float* __restrict__ rstd) {
   using C = Cols<T, MODE>;
-  constexpr int N = C::N, PIECES = C::PIECES, STAGES = NORM_STAGES<T, BIG, RMS>;
-  static_assert((BIG ? 1024 : LN_THREADS) * NORM_SMEM<T, BIG, RMS> + 2048 <= 227 * 1024, "shared memory of a block");
+  constexpr int N = C::N, PIECES = C::PIECES, STAGES = NORM_STAGES<T, SIZE == BIG, RMS>;
+  static_assert((SIZE == BIG ? 1024 : LN_THREADS) * NORM_SMEM<T, SIZE == BIG, RMS> + 2048 <= 227 * 1024, "shared memory of a block");
   extern __shared__ float4 kept4[];         // gains of every group, then (not RMS) biases, then the rows on their way
   __shared__ float2 red[2][32];
   const Group g(per_row);
@@ -222,7 +225,7 @@ k_layer_norm(const T* x, long long ld_x, long long nrows, int hidden, int per_ro
       for (int p = 0; p < PIECES; ++p)
 #pragma unroll
         for (int e = 0; e < N / 2; ++e) s = rows::add2(s, v[p][e]);
-      mu = group_sum<1>(make_float2(s.x + s.y, 0.f), g, red, turn).x * inv;
+      mu = group_sum<1, SIZE == PART>(make_float2(s.x + s.y, 0.f), g, red, turn).x * inv;
       s = make_float2(0.f, 0.f);
 #pragma unroll
       for (int p = 0; p < PIECES; ++p) {
@@ -241,7 +244,7 @@ k_layer_norm(const T* x, long long ld_x, long long nrows, int hidden, int per_ro
     for (int p = 0; p < PIECES; ++p)
 #pragma unroll
       for (int e = 0; e < N / 2; ++e) s = rows::fma2(v[p][e], v[p][e], s);
-    const float rs = 1.f / sqrtf(group_sum<1>(make_float2(s.x + s.y, 0.f), g, red, turn).x * inv + eps);
+    const float rs = 1.f / sqrtf(group_sum<1, SIZE == PART>(make_float2(s.x + s.y, 0.f), g, red, turn).x * inv + eps);
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       float2 w[N / 2], b[N / 2];
@@ -265,7 +268,7 @@ k_layer_norm(const T* x, long long ld_x, long long nrows, int hidden, int per_ro
 }
 
 // parts: per block the sums of dy h, then (want_bias) those of dy, `hidden` floats each.
-template <typename T, Mode MODE, int THREADS, bool RMS>
+template <typename T, Mode MODE, int THREADS, bool PARTS, bool RMS>
 __global__ void __launch_bounds__(THREADS, (GRAD_RESIDENT<T, MODE, RMS, THREADS>))
 k_layer_norm_grad(const T* dy, long long ld_dy, const T* x, long long ld_x, long long nrows, int hidden, int per_row, const void* gain,
                   int param_bf16, const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, long long ld_dx,
@@ -345,7 +348,7 @@ k_layer_norm_grad(const T* dy, long long ld_dy, const T* x, long long ld_x, long
         }
         if (!KEEP) asm volatile("" ::: "memory");     // one piece after the other: registers
       }
-      const float2 s = group_sum<RMS ? 1 : 2>(make_float2(along2.x + along2.y, level2.x + level2.y), g, red, turn);
+      const float2 s = group_sum<RMS ? 1 : 2, PARTS>(make_float2(along2.x + along2.y, level2.x + level2.y), g, red, turn);
       const float2 along = rows::both(-s.x * inv), level = rows::both(-s.y * inv);
 #pragma unroll
       for (int p = 0; p < PIECES; ++p) {
@@ -364,7 +367,7 @@ k_layer_norm_grad(const T* dy, long long ld_dy, const T* x, long long ld_x, long
   }
   // Groups of a warp that have the same columns by shuffles, then the groups (or warps) one after another.
   int turns = g.count, turn = g.id;
-  if (MODE != SHIFTED && g.threads < 32) {
+  if (PARTS && MODE != SHIFTED) {
     __syncwarp();
 #pragma unroll
     for (int o = 4; o < 32; o *= 2) {
@@ -439,18 +442,18 @@ k_layer_norm_params(const float* parts, int nparts, int width, int hidden, void*
 struct RowPlan {
   int per_row = 0, threads = 0, groups = 0;
   Mode mode = SINGLE;
-  bool big = false;
+  Size size = SOME;
 };
-RowPlan rows_of(long long hidden, size_t size, Mode mode) {
+RowPlan rows_of(long long hidden, size_t bytes, Mode mode) {
   RowPlan p;
-  const long long extent = hidden + (mode == SHIFTED ? 16 / (long long)size - 1 : 0);
-  if (extent > LN_MAX_HIDDEN) return rows_of(hidden, size, SINGLE);
+  const long long extent = hidden + (mode == SHIFTED ? 16 / (long long)bytes - 1 : 0);
+  if (extent > LN_MAX_HIDDEN) return rows_of(hidden, bytes, SINGLE);
   p.mode = mode;
   p.per_row = 4;
   while ((long long)p.per_row * LN_EACH < extent) p.per_row *= 2;
   p.threads = std::max(LN_THREADS, p.per_row);
   p.groups = p.threads / p.per_row;
-  p.big = p.per_row > LN_THREADS;
+  p.size = p.per_row < 32 ? PART : p.per_row > LN_THREADS ? BIG : SOME;
   return p;
 }
 // All groups get one row at most, or a number of groups that is a multiple of 8: then the rows of a group begin equally
@@ -462,37 +465,37 @@ long long blocks_for(const RowPlan& p, long long nrows, long long most, long lon
 }
 // Blocks of the backward pass: as many as are resident at once, and four rows at least for a group, since each block
 // writes its sums of dg and db.
-int grad_blocks(const RowPlan& p, long long nrows, bool rms, size_t size) {
-  const int resident = p.big ? 1 : rms && p.mode == ALIGNED && size == 2 ? GRAD_RESIDENT<__nv_bfloat16, ALIGNED, true, LN_THREADS> : GRAD_RESIDENT<float, SINGLE, false, LN_THREADS>;
+int grad_blocks(const RowPlan& p, long long nrows, bool rms, size_t bytes) {
+  const int resident = p.size == BIG ? 1 : rms && p.mode == ALIGNED && bytes == 2 ? GRAD_RESIDENT<__nv_bfloat16, ALIGNED, true, LN_THREADS> : GRAD_RESIDENT<float, SINGLE, false, LN_THREADS>;
   return (int)blocks_for(p, nrows, resident * LN_SMS / 8 * 8, 4);
 }
 
-template <typename T, Mode MODE, bool BIG, bool RMS>
+template <typename T, Mode MODE, Size SIZE, bool RMS>
 cudaError_t run_forward(const RowPlan& p, const void* x, long long ld_x, long long nrows, int hidden, const void* gain, const void* bias, int param_bf16,
                         float eps, void* y, long long ld_y, float* mean, float* rstd, cudaStream_t st) {
-  const size_t smem = p.threads * NORM_SMEM<T, BIG, RMS>;
-  const cudaError_t e = cudaFuncSetAttribute(k_layer_norm<T, MODE, BIG, RMS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             (int)((BIG ? 1024 : LN_THREADS) * NORM_SMEM<T, BIG, RMS>));
+  const size_t smem = p.threads * NORM_SMEM<T, SIZE == BIG, RMS>;
+  const cudaError_t e = cudaFuncSetAttribute(k_layer_norm<T, MODE, SIZE, RMS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)((SIZE == BIG ? 1024 : LN_THREADS) * NORM_SMEM<T, SIZE == BIG, RMS>));
   if (e != cudaSuccess) return e;
   // four times as many blocks as are resident, since SMs far from the memory take longer (32768 rows of 4096, bf16: 100 us
   // with four blocks per SM in all, 89 with 16, 96 with 32)
-  const unsigned blocks = (unsigned)blocks_for(p, nrows, (p.big ? 4 : 16) * LN_SMS, 1);
-  k_layer_norm<T, MODE, BIG, RMS><<<blocks, p.threads, smem, st>>>((const T*)x, ld_x, nrows, hidden, p.per_row, gain, bias, param_bf16, eps, (T*)y, ld_y, mean, rstd);
+  const unsigned blocks = (unsigned)blocks_for(p, nrows, (SIZE == BIG ? 4 : 16) * LN_SMS, 1);
+  k_layer_norm<T, MODE, SIZE, RMS><<<blocks, p.threads, smem, st>>>((const T*)x, ld_x, nrows, hidden, p.per_row, gain, bias, param_bf16, eps, (T*)y, ld_y, mean, rstd);
   return cudaGetLastError();
 }
-template <typename T, Mode MODE, int THREADS, bool RMS>
+template <typename T, Mode MODE, int THREADS, bool PARTS, bool RMS>
 cudaError_t run_backward_of(const RowPlan& p, const void* dy, long long ld_dy, const void* x, long long ld_x, long long nrows, int hidden, const void* gain,
                             int param_bf16, const float* mean, const float* rstd, void* dx, long long ld_dx, float* parts, int want_bias, cudaStream_t st) {
-  const cudaError_t e = cudaFuncSetAttribute(k_layer_norm_grad<T, MODE, THREADS, RMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(THREADS * GRAD_SMEM<T, THREADS>));
+  const cudaError_t e = cudaFuncSetAttribute(k_layer_norm_grad<T, MODE, THREADS, PARTS, RMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(THREADS * GRAD_SMEM<T, THREADS>));
   if (e != cudaSuccess) return e;
-  k_layer_norm_grad<T, MODE, THREADS, RMS><<<grad_blocks(p, nrows, RMS, sizeof(T)), p.threads, p.threads * GRAD_SMEM<T, THREADS>, st>>>(
+  k_layer_norm_grad<T, MODE, THREADS, PARTS, RMS><<<grad_blocks(p, nrows, RMS, sizeof(T)), p.threads, p.threads * GRAD_SMEM<T, THREADS>, st>>>(
       (const T*)dy, ld_dy, (const T*)x, ld_x, nrows, hidden, p.per_row, gain, param_bf16, mean, rstd, (T*)dx, ld_dx, parts, want_bias);
   return cudaGetLastError();
 }
-template <typename T, Mode MODE, bool BIG, bool RMS, typename... A>
+template <typename T, Mode MODE, Size SIZE, bool RMS, typename... A>
 cudaError_t run_backward(const RowPlan& p, A... a) {
-  if constexpr (!BIG) return run_backward_of<T, MODE, LN_THREADS, RMS>(p, a...);
-  else return p.per_row == 512 ? run_backward_of<T, MODE, 512, RMS>(p, a...) : run_backward_of<T, MODE, 1024, RMS>(p, a...);
+  if constexpr (SIZE != BIG) return run_backward_of<T, MODE, LN_THREADS, SIZE == PART, RMS>(p, a...);
+  else return p.per_row == 512 ? run_backward_of<T, MODE, 512, false, RMS>(p, a...) : run_backward_of<T, MODE, 1024, false, RMS>(p, a...);
 }
 
 fira_status check_norm(const std::string& who, int64_t rows, int64_t hidden, fira_dtype dtype, fira_dtype param_dtype) {
@@ -517,8 +520,9 @@ Mode mode_of(const void* a, long long ld, long long hidden, size_t size, bool al
 
 #define LN_DISPATCH_MODE(CALL, T, M)                                                                                    \
   do {                                                                                                                  \
-    if (p.big) { if (rms) CALL(T, M, true, true); else CALL(T, M, true, false); }                                       \
-    else { if (rms) CALL(T, M, false, true); else CALL(T, M, false, false); }                                           \
+    if (p.size == BIG) { if (rms) CALL(T, M, BIG, true); else CALL(T, M, BIG, false); }                                 \
+    else if (p.size == PART) { if (rms) CALL(T, M, PART, true); else CALL(T, M, PART, false); }                         \
+    else { if (rms) CALL(T, M, SOME, true); else CALL(T, M, SOME, false); }                                             \
   } while (0)
 #define LN_DISPATCH_TYPE(CALL, T)                                                                                       \
   do {                                                                                                                  \
