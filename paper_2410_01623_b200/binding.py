@@ -14,6 +14,12 @@ from typing import Optional, Sequence, Tuple
 
 import torch
 
+try:                                           # lists of tensors read natively (csrc/grad_list.cpp): speed alone
+    from ._native_lists import grad_list as _native_grad_list
+except ImportError:
+    def _native_grad_list(Gs, out):
+        return None
+
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libfira.so")
 
@@ -97,7 +103,7 @@ SIGNATURES = {
                                   C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.POINTER(C.c_int64), C.c_int,
                                   C.c_int64, C.c_float, C.c_void_p]),
     "fira_grad_work_bytes": (C.c_size_t, [C.c_int32]),
-    # (host arrays by address: GradDesc and device pointers)
+    # (host arrays as bytes objects, or by address: GradDesc and device pointers)
     "fira_grad_norm": (C.c_int, [C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "fira_clip_grads": (C.c_int, [C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p,
                                   C.c_void_p, C.c_size_t, C.c_void_p]),
@@ -251,8 +257,11 @@ def _grad_codes(tensors: Sequence[torch.Tensor]):
 
 
 def _grad_list(Gs: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]]):
-    """The device's index and the arrays that go to the library: descriptors, addresses, the outputs' addresses.  Whole
-    lists go through map() and arrays: a small list is bound by this."""
+    """The device's index and what goes to the library: descriptors, addresses, the outputs' addresses.  Contiguous
+    tensors are read natively; the others' lists go through map() and arrays."""
+    native = _native_grad_list(Gs, out)
+    if native is not None:
+        return native
     n = len(Gs)
     if n == 0:
         raise ValueError("an empty list of gradients")
@@ -282,7 +291,8 @@ def _grad_list(Gs: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]]
     index = devices.pop()
     if index < 0:
         raise ValueError(f"the Fira library runs on a CUDA device only, not on {Gs[0].device}")
-    return index, words, array("Q", map(_T.data_ptr, Gs)), None if out is None else array("Q", map(_T.data_ptr, out))
+    return (index, words.tobytes(), array("Q", map(_T.data_ptr, Gs)).tobytes(),
+            None if out is None else array("Q", map(_T.data_ptr, out)).tobytes())
 
 
 def grad_work_bytes(count: int) -> int:
@@ -303,8 +313,7 @@ def grad_norm(Gs: Sequence[torch.Tensor], work: Optional[torch.Tensor] = None) -
         work = norm.new_empty(L.fira_grad_work_bytes(n) // 4)
     elif work.get_device() != index:
         raise ValueError(f"work is on {work.device}, the gradients on {norm.device}")
-    status = L.fira_grad_norm(n, words.buffer_info()[0], at.buffer_info()[0], norm.data_ptr(), work.data_ptr(),
-                              work.nbytes, _raw_stream(index))
+    status = L.fira_grad_norm(n, words, at, norm.data_ptr(), work.data_ptr(), work.nbytes, _raw_stream(index))
     if status:
         check(status)
     return norm
@@ -328,9 +337,8 @@ def clip_grads(Gs: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequen
     elif work.get_device() != index:
         raise ValueError(f"work is on {work.device}, the gradients on {norm.device}")
     scale = torch.empty_like(norm)
-    status = L.fira_clip_grads(n, words.buffer_info()[0], at.buffer_info()[0],
-                               None if out_at is None else out_at.buffer_info()[0], max_norm, norm.data_ptr(),
-                               scale.data_ptr(), work.data_ptr(), work.nbytes, _raw_stream(index))
+    status = L.fira_clip_grads(n, words, at, out_at, max_norm, norm.data_ptr(), scale.data_ptr(), work.data_ptr(),
+                               work.nbytes, _raw_stream(index))
     if status:
         check(status)
     return norm, scale

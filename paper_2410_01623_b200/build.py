@@ -1,9 +1,10 @@
-"""Builds libfira.so (the C-ABI library) in-tree with nvcc for sm_100a."""
+"""Builds libfira.so (the C-ABI library) in-tree with nvcc for sm_100a, and the binding's reading of tensor lists."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
@@ -12,6 +13,30 @@ SOURCES = ["fira_api.cu", "step_simt.cu", "step_tc.cu", "refresh.cu", "part_gemm
            "grad_clip.cu", "embedding.cu", "layer_norm.cu"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--expt-relaxed-constexpr"]
+
+
+LISTS_PATH = os.path.join(PKG_DIR, "_native_lists.so")      # the binding's reading of tensor lists (grad_list.cpp)
+
+
+def _build_lists(force: bool) -> None:
+    """Compiles the binding's reading of tensor lists against torch's headers.  It is a matter of speed alone: where it
+    cannot be built, that is said, and the binding reads lists in Python."""
+    src = os.path.join(CSRC, "grad_list.cpp")
+    if not force and os.path.exists(LISTS_PATH) and os.path.getmtime(LISTS_PATH) >= os.path.getmtime(src):
+        return
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{root}/include",
+           f"-I{root}/include/torch/csrc/api/include", f"-I{sysconfig.get_paths()['include']}", src, "-o", LISTS_PATH,
+           f"-L{root}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", f"-Wl,-rpath,{root}/lib"]
+    try:
+        done = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        said = done.stdout if done.returncode else None
+    except OSError as e:
+        said = str(e)
+    if said is not None:
+        sys.stderr.write(f"--- not built: {LISTS_PATH} (lists of tensors are read in Python)\n{said}\n")
 
 
 def _nvcc() -> str:
@@ -23,7 +48,7 @@ def needs_build() -> bool:
     if not os.path.exists(LIB_PATH):
         return True
     t = os.path.getmtime(LIB_PATH)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
+    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if not f.endswith(".cpp")]
     deps.append(os.path.join(os.path.dirname(PKG_DIR), "include", "fira.h"))
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -31,6 +56,7 @@ def needs_build() -> bool:
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compiles every .cu of the library to objects (in parallel) and links the
     shared library next to this file.  Returns the library path."""
+    _build_lists(force)
     if not force and not needs_build():
         return LIB_PATH
     obj_dir = os.path.join(PKG_DIR, "_build")

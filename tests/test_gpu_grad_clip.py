@@ -96,6 +96,26 @@ def test_pitched_rows(dtype, out_dtype, rows, cols, pitch, out_pitch):
     assert bool(wide[:, cols:].isnan().all())
 
 
+def test_lists_read_natively_and_in_python_are_the_same(monkeypatch):
+    """The two ways to the library's arrays; what the native one leaves to the other, it does not touch."""
+    pytest.importorskip("paper_2410_01623_b200._native_lists")
+    gen = torch.Generator().manual_seed(7)
+    f32 = [torch.randn(s, generator=gen).cuda() for s in ((3, 4), (7,), (0,), (), (2, 3, 5))]
+    mixed = [g.to([torch.float32, torch.bfloat16][i % 2]) for i, g in enumerate(f32)]
+    cases = [(f32, None), (mixed, None), (tuple(mixed), f32), (f32, [g.bfloat16() for g in f32])]
+    native = [fb._native_grad_list(*c) for c in cases]
+    assert all(x is not None and len(x) == 4 for x in native)
+    flat = torch.zeros(4, 6, device="cuda")
+    for other in ([flat[:, :3]], [flat.t()], [flat.half()], [flat.cpu()], [flat, flat.cpu()], [], iter([flat]), [1], [None]):
+        assert fb._native_grad_list(other, None) is None
+    assert fb._native_grad_list([flat], [flat.t()]) is None and fb._native_grad_list([flat], []) is None
+    monkeypatch.setattr(fb, "_native_grad_list", lambda Gs, out: None)
+    assert [fb._grad_list(*c) for c in cases] == native
+    norm = fb.grad_norm(mixed)
+    monkeypatch.undo()
+    assert float(fb.grad_norm(mixed)) == float(norm)
+
+
 def test_transposed_and_column_sliced_gradients():
     gen = torch.Generator().manual_seed(6)
     whole = torch.randn(96, 80, generator=gen).cuda()
