@@ -283,6 +283,11 @@ k_layer_norm_grad(const T* dy, long long ld_dy, const T* x, long long ld_x, long
   const Group g(per_row);
   const long long stride = (long long)gridDim.x * g.count;
   long long row = (long long)blockIdx.x * g.count + g.id;
+  if (PARTS && MODE == SHIFTED) {           // the groups of a warp eight rows apart: they begin alike, and have the same columns
+    const int groups = 32 / g.threads;
+    const long long warp = (long long)blockIdx.x * (THREADS / 32) + threadIdx.x / 32;
+    row = (warp / 8 * groups + g.id % groups) * 8 + warp % 8;
+  }
   const C cols(g, hidden, MODE == SHIFTED ? shift_of(x + row * ld_x) : 0);
   float2 dg[PIECES][N / 2], db[PIECES][N / 2];
 #pragma unroll
@@ -365,9 +370,9 @@ k_layer_norm_grad(const T* dy, long long ld_dy, const T* x, long long ld_x, long
       stage = stage + 1 == STAGES ? 0 : stage + 1;
     }
   }
-  // Groups of a warp that have the same columns by shuffles, then the groups (or warps) one after another.
+  // Groups of a warp (which have the same columns) by shuffles, then the groups, or the warps, one after another.
   int turns = g.count, turn = g.id;
-  if (PARTS && MODE != SHIFTED) {
+  if (PARTS) {
     __syncwarp();
 #pragma unroll
     for (int o = 4; o < 32; o *= 2) {

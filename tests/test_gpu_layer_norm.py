@@ -74,7 +74,7 @@ def check_backward(dY, x, gain, mean, rstd, rms, dX, dgain, dbias, old=None):
         assert within(got, want, allow), name
 
 
-SHAPES = [(1, 1), (3, 2), (5, 7), (4, 8), (33, 64), (100, 255), (64, 256), (9, 257), (130, 512), (50, 1000), (300, 1024), (77, 1707),
+SHAPES = [(1529, 43), (1000, 21), (700, 100), (333, 200), (4097, 33), (1, 1), (3, 2), (5, 7), (4, 8), (33, 64), (100, 255), (64, 256), (9, 257), (130, 512), (50, 1000), (300, 1024), (77, 1707),
           (40, 2048), (21, 4096), (10, 4100), (6, 5461), (5, 8192), (4, 8200), (3, 11008), (2, 16384), (2, 16383)]
 
 
