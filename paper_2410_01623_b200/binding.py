@@ -8,17 +8,13 @@ library is missing, `lib()` raises; there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
+import importlib
 import os
+import sysconfig
 from array import array
 from typing import Optional, Sequence, Tuple
 
 import torch
-
-try:                                           # lists of tensors read natively (csrc/grad_list.cpp): speed alone
-    from ._native_lists import grad_list as _native_grad_list
-except ImportError:
-    def _native_grad_list(Gs, out):
-        return None
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libfira.so")
@@ -254,6 +250,25 @@ def _grad_codes(tensors: Sequence[torch.Tensor]):
     if not types <= _CODES.keys():
         raise ValueError(f"gradients and their outputs are float32 or bfloat16, not {types}")
     return _CODES[types.pop()] if len(types) == 1 else array("i", [_CODES[t.dtype] for t in tensors])
+
+
+_LISTS_PATH = os.path.join(_PKG, "_native_lists" + sysconfig.get_config_var("EXT_SUFFIX"))
+
+
+def _native_grad_list(Gs, out):
+    """Lists of tensors read natively (csrc/grad_list.cpp): speed alone.  The module may be built after this one is imported, so
+    it is looked for until it is there; one that is made for other descriptors or another torch is not used."""
+    global _native_grad_list
+    if not os.path.exists(_LISTS_PATH):
+        return None
+    importlib.invalidate_caches()
+    try:
+        module = importlib.import_module("._native_lists", __package__)
+        fits = (module.torch_version, module.desc_bytes) == (torch.__version__, C.sizeof(GradDesc))
+    except (ImportError, AttributeError):
+        fits = False
+    _native_grad_list = module.grad_list if fits else lambda Gs, out: None
+    return _native_grad_list(Gs, out)
 
 
 def _grad_list(Gs: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]]):

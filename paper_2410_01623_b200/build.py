@@ -1,6 +1,8 @@
 """Builds libfira.so (the C-ABI library) in-tree with nvcc for sm_100a, and the binding's reading of tensor lists."""
 from __future__ import annotations
 
+import glob
+import hashlib
 import os
 import subprocess
 import sys
@@ -15,20 +17,40 @@ NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--expt-relaxed-constexpr"]
 
 
-LISTS_PATH = os.path.join(PKG_DIR, "_native_lists.so")      # the binding's reading of tensor lists (grad_list.cpp)
+# The binding's reading of tensor lists (grad_list.cpp), named for the interpreter that it is built for.
+LISTS_PATH = os.path.join(PKG_DIR, "_native_lists" + sysconfig.get_config_var("EXT_SUFFIX"))
+LISTS_KEY_PATH = os.path.join(PKG_DIR, "_build", "native_lists.key")
+HEADER = os.path.join(os.path.dirname(PKG_DIR), "include", "fira.h")
+
+
+def _lists_key(torch) -> str:
+    """What the module is made from: its source, the header whose descriptors it writes, torch and the interpreter."""
+    key = hashlib.sha256()
+    for path in (os.path.join(CSRC, "grad_list.cpp"), HEADER):
+        with open(path, "rb") as f:
+            key.update(f.read() + b"\0")
+    key.update(f"{torch.__version__} {int(torch._C._GLIBCXX_USE_CXX11_ABI)} {os.path.basename(LISTS_PATH)}".encode())
+    return key.hexdigest()
 
 
 def _build_lists(force: bool) -> None:
-    """Compiles the binding's reading of tensor lists against torch's headers.  It is a matter of speed alone: where it
-    cannot be built, that is said, and the binding reads lists in Python."""
-    src = os.path.join(CSRC, "grad_list.cpp")
-    if not force and os.path.exists(LISTS_PATH) and os.path.getmtime(LISTS_PATH) >= os.path.getmtime(src):
-        return
+    """Compiles the binding's reading of tensor lists against torch's headers, anew where anything that it is made from has
+    changed.  It is a matter of speed alone: where it cannot be built, that is said, nothing older is left in its place, and
+    the binding reads lists in Python."""
     import torch
-    root = os.path.dirname(torch.__file__)
+    key = _lists_key(torch)
+    if not force and os.path.exists(LISTS_PATH) and os.path.exists(LISTS_KEY_PATH):
+        with open(LISTS_KEY_PATH) as f:
+            if f.read() == key:
+                return
+    for old in glob.glob(os.path.join(os.path.dirname(LISTS_PATH), "_native_lists*.so")) + [LISTS_KEY_PATH]:
+        if os.path.exists(old):
+            os.remove(old)
+    root, made = os.path.dirname(torch.__file__), f"{LISTS_PATH}.{os.getpid()}"
     cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{root}/include",
-           f"-I{root}/include/torch/csrc/api/include", f"-I{sysconfig.get_paths()['include']}", src, "-o", LISTS_PATH,
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DFIRA_LISTS_TORCH="{torch.__version__}"',
+           f"-I{root}/include", f"-I{root}/include/torch/csrc/api/include", f"-I{sysconfig.get_paths()['include']}",
+           os.path.join(CSRC, "grad_list.cpp"), "-o", made,
            f"-L{root}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", f"-Wl,-rpath,{root}/lib"]
     try:
         done = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
@@ -36,7 +58,14 @@ def _build_lists(force: bool) -> None:
     except OSError as e:
         said = str(e)
     if said is not None:
+        if os.path.exists(made):
+            os.remove(made)
         sys.stderr.write(f"--- not built: {LISTS_PATH} (lists of tensors are read in Python)\n{said}\n")
+        return
+    os.replace(made, LISTS_PATH)
+    os.makedirs(os.path.dirname(LISTS_KEY_PATH), exist_ok=True)
+    with open(LISTS_KEY_PATH, "w") as f:
+        f.write(key)
 
 
 def _nvcc() -> str:
@@ -49,7 +78,7 @@ def needs_build() -> bool:
         return True
     t = os.path.getmtime(LIB_PATH)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if not f.endswith(".cpp")]
-    deps.append(os.path.join(os.path.dirname(PKG_DIR), "include", "fira.h"))
+    deps.append(HEADER)
     return any(os.path.getmtime(d) > t for d in deps)
 
 

@@ -65,4 +65,12 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native_lists", nullptr, -1, metho
 
 }  // namespace
 
-extern "C" __attribute__((visibility("default"))) PyObject* PyInit__native_lists() { return PyModule_Create(&module); }
+// With what binding.py holds against its own before it uses the module: torch's version and the size of a descriptor.
+extern "C" __attribute__((visibility("default"))) PyObject* PyInit__native_lists() {
+  PyObject* m = PyModule_Create(&module);
+  if (m && (PyModule_AddStringConstant(m, "torch_version", FIRA_LISTS_TORCH) < 0 || PyModule_AddIntConstant(m, "desc_bytes", sizeof(fira_grad_desc)) < 0)) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}
