@@ -204,6 +204,12 @@ def _device_of(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
     return index
 
 
+def _check_work(work: Optional[torch.Tensor]) -> None:
+    """A workspace is as large as its elements say: an expanded tensor is not."""
+    if work is not None and not work.is_contiguous():
+        raise ValueError(f"work: a contiguous tensor is needed, not strides {tuple(work.stride())} of shape {tuple(work.shape)}")
+
+
 def _pitch(t: torch.Tensor, what: str) -> int:
     """Elements from row to row of a tensor whose last dimension is a row."""
     if t.is_contiguous():
@@ -318,6 +324,7 @@ def grad_norm(Gs: Sequence[torch.Tensor], work: Optional[torch.Tensor] = None) -
     """fira_grad_norm: the norm over all elements of a list of gradients (float32 and bfloat16 may be mixed), as a
     float32 tensor of one element on the device; nothing waits for it.  work: a byte tensor of at least
     grad_work_bytes(len(Gs)) bytes; by default torch's allocator lends one for the call."""
+    _check_work(work)
     index, words, at, _ = _grad_list(Gs, None)
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):
@@ -341,6 +348,7 @@ def clip_grads(Gs: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequen
     tensors of one element on the device.  work: as for grad_norm."""
     if out is not None and len(out) != len(Gs):
         raise ValueError(f"{len(out)} outputs for {len(Gs)} gradients")
+    _check_work(work)
     index, words, at, out_at = _grad_list(Gs, out)
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):
@@ -399,6 +407,7 @@ def embedding_grad(tokens: torch.Tensor, dY: torch.Tensor, vocab: int, scale: fl
         raise ValueError(f"dY {tuple(dY.shape)} for tokens {tuple(tokens.shape)} of a vocabulary of {vocab}")
     if accumulate and out is None:
         raise ValueError("accumulate: out is needed")
+    _check_work(work)
     hidden = dY.shape[-1]
     index = _device_of(dY, tokens, out, work)
     if index != torch.cuda.current_device():
@@ -496,6 +505,7 @@ def layer_norm_grad(dY: torch.Tensor, x: torch.Tensor, gain: torch.Tensor, mean:
         raise ValueError("the form without mean has no bias")
     if accumulate and (dgain is None or (dbias is None and not rms)):
         raise ValueError("accumulate: dgain and dbias are needed")
+    _check_work(work)
     ld = 0 if x.is_contiguous() else _pitch(x, "x")
     index = _device_of(x, dY, gain, mean, rstd, out, dgain, dbias, work)
     if index != torch.cuda.current_device():
