@@ -351,12 +351,12 @@ k_token_gather(const int2* entries, const int* counts, const int* fronts, int ti
                int* total) {
   extern __shared__ __align__(16) unsigned shared[];      // counts [warps][nrows], lists [warps][ORD_LIST] of (position, token)
   __shared__ unsigned below_s[32], sum_s[32];
-  ptx::grid_launch_next();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, threads = blockDim.x;
   const unsigned me = blockIdx.x, mask = gridDim.x - 1, dealt = FINE ? me & (unsigned)(split - 1) : me;
   for (int i = threadIdx.x; i < warps * nrows; i += threads) shared[i] = 0;
   __syncthreads();
   ptx::grid_wait();
+  ptx::grid_launch_next();                  // (behind the wait: the next kernel may rely on k_token_split too)
   counts += (long long)dealt * tiles;
   fronts += (long long)dealt * tiles;
   unsigned below = 0;                       // tokens of lower remainders: of all dealt in front of this one's, and of those dealt with it
