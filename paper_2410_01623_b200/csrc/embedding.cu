@@ -424,8 +424,13 @@ k_token_gather(const int2* entries, const int* counts, const int* fronts, int ti
 constexpr int TG_DEPTH = 4;                 // rows of dY of a warp on their way
 constexpr int TG_MIN = 8;                   // positions of a stretch at least
 constexpr int TG_GROUP = 16;                // stretches whose parts of a long row are added by one warp
-constexpr int TG_ZERO_ROWS = 64;            // rows that a block looks over for tokens, or TG_ZERO_MOST, where looking costs more
-constexpr int TG_ZERO_MOST = 256;           // (16384 tokens, hidden 512, fp32: 31.8 us with 64 rows, 29.6 with 256; 32768 tokens: 41 and 51)
+// Rows that a block looks over for tokens: TG_ZERO_ROWS, or TG_ZERO_MOST where looking takes longer than zeroing: blocks that look
+// through all tokens, and rows of 1024 bytes, up to 1536 with the number of tokens.  (us a call with 64 and with 256, fp32, at 512, 4096 and 16384
+// tokens of a vocabulary of 32000: hidden 64 10.1 and 9.5, 14.1 and 13.9, 20.4 and 19.8; 256 12.8 and 11.1, 14.9 and 13.6, 21.5 and 19.5; 512 17.5 and 13.8,
+// 19.2 and 20.3, 28.3 and 27.3; 1024 27 and 40, 31 and 42, 45 and 52; 4096 85 and 153, 95 and 159, 135 and 194.  Of 128000, hidden 64: 19 and 15, 23 and 19,
+// 34 and 23; hidden 384: 37 and 39, 43 and 42, 54 and 48.  bf16, of 32000, hidden 768: 16 and 14, 18 and 17, 26 and 24)
+constexpr int TG_ZERO_ROWS = 64;
+constexpr int TG_ZERO_MOST = 256;
 constexpr int TG_ZERO_EARLY = 16384;        // tokens up to which such a block looks through them itself (1024: 20.8 us, or 21.9; 16384: 31.0 and 32.1)
 
 struct TablePlan {
@@ -539,7 +544,9 @@ struct Slice {
   }
 };
 
-__host__ __device__ constexpr int zero_rows_of(int ntokens) { return ntokens > 4096 && ntokens <= TG_ZERO_EARLY ? TG_ZERO_MOST : TG_ZERO_ROWS; }
+__host__ __device__ constexpr int zero_rows_of(int ntokens, long long row_bytes) {
+  return ntokens <= TG_ZERO_EARLY && row_bytes <= (ntokens < 4096 ? 1024 + ntokens / 8 : 1536) ? TG_ZERO_MOST : TG_ZERO_ROWS;
+}
 
 // Zeroes the rows of `first` on that no token names.  early: in front of the wait for k_token_order, from the tokens.
 template <typename TO, typename TOK, bool ALIGNED>
@@ -593,7 +600,7 @@ k_table_grad(const int2* order, const int2* span, const int* total, unsigned* co
   const bool early = ntokens <= TG_ZERO_EARLY;
   const int main_blocks = gridDim.x - zero_blocks, block = early ? (int)blockIdx.x - zero_blocks : (int)blockIdx.x;
   if (block < 0 || block >= main_blocks) {
-    const int each = zero_rows_of(ntokens);
+    const int each = zero_rows_of(ntokens, (long long)hidden * sizeof(TO));
     zero_rows<TO, TOK, ALIGNED>((long long)(early ? blockIdx.x : block - main_blocks) * each, each, vocab, hidden, span, tokens, ntokens, early, G, ldg);
     ptx::grid_wait();                       // (this kernel does not end before the one in front of it)
     return;
@@ -817,7 +824,7 @@ cudaError_t run_order(const TablePlan& p, const void* tokens, int n, int vocab, 
 template <typename TI, typename TO, typename TOK>
 cudaError_t run_grad(const TablePlan& p, const void* tokens, int n, const void* dY, long long ld, int vocab, int hidden, float scale, int add, void* G, long long ldg, char* work,
                      bool vector, cudaStream_t st) {
-  const int zero_blocks = add ? 0 : (vocab + zero_rows_of(n) - 1) / zero_rows_of(n);
+  const int zero_rows_each = zero_rows_of(n, (long long)hidden * sizeof(TO)), zero_blocks = add ? 0 : (vocab + zero_rows_each - 1) / zero_rows_each;
   const dim3 grid((unsigned)(zero_blocks + (p.chunks * p.slices + EM_WARPS - 1) / EM_WARPS));
   if (grid.x == 0) return cudaSuccess;
   auto kernel = p.pieces == 2 ? (vector ? k_table_grad<TI, TO, TOK, true, 2> : k_table_grad<TI, TO, TOK, false, 2>)
