@@ -36,9 +36,10 @@ __device__ __forceinline__ int token_at(const TOK* tokens, long long i, int voca
 }
 
 // Wide rows of whole 16-byte units on 16-byte boundaries: a warp takes LK_ROWS positions and a slice of 32 units.
-// (131072 rows of 1024, bf16: 55 us; by k_embedding_words 64.  Of 64, fp32: 10.3 and 9.7.)
+// (131072 rows of 1024, bf16: 55 us; by k_embedding_words 64.  Of 64, fp32: 10.3 and 9.7.)  Eight blocks to an SM: 65536 rows of 1024, bf16, 36.4 us;
+// with the 34 registers that the compiler takes otherwise, 37.2.
 template <typename T, typename TOK>
-__global__ void __launch_bounds__(EM_THREADS)
+__global__ void __launch_bounds__(EM_THREADS, 8)
 k_embedding_rows(const T* __restrict__ table, long long ld, const TOK* __restrict__ tokens, long long n, int vocab, int hidden, int slices,
                  float scale, T* __restrict__ out, long long ld_out) {
   constexpr int N = rows::PER16<T>;
@@ -55,10 +56,11 @@ k_embedding_rows(const T* __restrict__ table, long long ld, const TOK* __restric
 #pragma unroll
   for (int u = 0; u < LK_ROWS; ++u) {
     if (i0 + u >= n) break;
+    const float by = t[u] >= 0 ? scale : 0.f;          // (a row of zeros whatever the factor)
     float2 v[N / 2];
     rows::unpack<T>(a[u], v);
 #pragma unroll
-    for (int e = 0; e < N / 2; ++e) v[e] = rows::mul2(v[e], rows::both(scale));
+    for (int e = 0; e < N / 2; ++e) v[e] = rows::mul2(v[e], rows::both(by));
     *reinterpret_cast<uint4*>(out + (i0 + u) * ld_out + col) = rows::pack<T>(v);
   }
 }
@@ -82,15 +84,17 @@ k_embedding_words(const T* __restrict__ table, long long ld, const TOK* __restri
   uint4 a[LK_EACH][W + (ALIGNED ? 0 : 1)];
   T* to[LK_EACH];                           // the first word, and the column of its first element (hidden: none)
   int col[LK_EACH], skip[LK_EACH];
+  bool none[LK_EACH];                       // no token: a row of zeros, whatever the factor
 #pragma unroll
   for (int u = 0; u < LK_EACH; ++u) {
     const unsigned x = item0 + u * EM_THREADS + threadIdx.x, down = x / items;      // (items < 2^23: no overflow)
     const long long i = row0 + down;
 #pragma unroll
     for (int w = 0; w < W + (ALIGNED ? 0 : 1); ++w) a[u][w] = make_uint4(0u, 0u, 0u, 0u);
-    col[u] = hidden; skip[u] = 0; to[u] = out;
+    col[u] = hidden; skip[u] = 0; to[u] = out; none[u] = true;
     if (i >= n) continue;
     const int t = token_at(tokens, i, vocab);
+    none[u] = t < 0;
     T* out_row = out + i * ld_out;
     const T* row = table + (long long)max(t, 0) * ld;
     col[u] = (int)(x - down * items) * (N * W);
@@ -116,10 +120,11 @@ k_embedding_words(const T* __restrict__ table, long long ld, const TOK* __restri
       uint4 x = a[u][w];
       if constexpr (!ALIGNED) x = rows::funnel16(a[u][w], a[u][w + 1], skip[u]);
       if (scale != 1.f) {
+        const float by = none[u] ? 0.f : scale;
         float2 v[N / 2];
         rows::unpack<T>(x, v);
 #pragma unroll
-        for (int e = 0; e < N / 2; ++e) v[e] = rows::mul2(v[e], rows::both(scale));
+        for (int e = 0; e < N / 2; ++e) v[e] = rows::mul2(v[e], rows::both(by));
         x = rows::pack<T>(v);
       }
       if (ALIGNED) {
