@@ -29,7 +29,10 @@ constexpr int GC_BLOCKS = GC_SMS * 4;             // blocks of the sums, all res
 constexpr int GC_SCALE_BLOCKS = GC_SMS * 32;      // of the scaling: eight times as many as are resident, since SMs far from the
                                                   // memory take longer (2.7 GB of bf16: 925 us with 4 per SM, 831 so, as long as a copy)
 constexpr int GC_MANY = 480, GC_FEW = 48;         // tensors of a launch: 31 KB of kernel arguments, or 3.1 KB
-constexpr long long GC_KEPT = 48ll << 20;         // bytes that the sums leave in L2 for the scaling (232 MB of fp32: 110 -> 104 us)
+// Bytes of a list that the sums leave in L2 for the scaling (232 MB of fp32: 110 -> 104 us; 1440 bf16 tensors of 60000, three launches with
+// 48 MB each 156 us, with 48 in all 147).  In place with a factor of 1 nothing reads them again, and they stay: the optimizer step that
+// follows takes the same time (350 us to 1.35 ms, both types), ten passes over another 80 MB that L2 would hold up to 209 us instead of 176.
+constexpr long long GC_KEPT = 48ll << 20;
 
 // One tensor.  A flat one is one row; rows of a pitched one start on their own.
 struct GradEntry {
@@ -420,14 +423,21 @@ void fill(GradTable<CAP>& tab, int base, int n, const fira_grad_desc* descs, con
   tab.tiles = (int)tiles;
 }
 
-// The first tile from which on the list's bytes fit what the L2 is expected to keep.
+// Bytes of the tensors from `from` on, as far as they matter: what is left of GC_KEPT for those in front of them.
+long long kept_in_front_of(int32_t from, int32_t count, const fira_grad_desc* descs) {
+  long long left = GC_KEPT;
+  for (int32_t i = count; i-- > from && left > 0;) left -= descs[i].rows * descs[i].cols * (descs[i].dtype == FIRA_BF16 ? 2 : 4);
+  return std::max(left, 0ll);
+}
+
+// The first tile from which on a launch's bytes fit what the L2 is expected to keep of them.
 template <int CAP>
-int kept_from(const GradTable<CAP>& tab) {
+int kept_from(const GradTable<CAP>& tab, long long kept) {
   long long bytes = 0;
   for (int q = tab.count - 1; q >= 0; --q) {
     const long long per_tile = (long long)GC_TILE * (tab.t[q].single ? 1 : GC_CHUNK) * (tab.t[q].bf16 ? 2 : 4);
     const long long tiles = (q + 1 < tab.count ? tab.t[q + 1].tile_start : tab.tiles) - tab.t[q].tile_start;
-    if (bytes + tiles * per_tile > GC_KEPT) return tab.t[q].tile_start + (int)(tiles - (GC_KEPT - bytes) / per_tile);
+    if (bytes + tiles * per_tile > kept) return tab.t[q].tile_start + (int)(tiles - (kept - bytes) / per_tile);
     bytes += tiles * per_tile;
   }
   return 0;
@@ -442,7 +452,7 @@ cudaError_t run_list(int32_t count, const fira_grad_desc* descs, const void* con
   for (int base = 0; base < count; base += CAP) {
     fill(tab, base, std::min(CAP, count - base), descs, G_dev, out_dev);
     const int blocks = std::max(1, std::min(GC_BLOCKS, tab.tiles));
-    k_grad_squares<CAP><<<blocks, GC_THREADS, 0, st>>>(tab, sums + nsums, scale_dev ? kept_from(tab) : tab.tiles);
+    k_grad_squares<CAP><<<blocks, GC_THREADS, 0, st>>>(tab, sums + nsums, scale_dev ? kept_from(tab, kept_in_front_of(std::min(count, base + CAP), count, descs)) : tab.tiles);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     nsums += blocks;
