@@ -210,20 +210,49 @@ def _check_work(work: Optional[torch.Tensor]) -> None:
         raise ValueError(f"work: a contiguous tensor is needed, not strides {tuple(work.stride())} of shape {tuple(work.shape)}")
 
 
-def _pitch(t: torch.Tensor, what: str) -> int:
-    """Elements from row to row of a tensor whose last dimension is a row."""
+def _pitch_of(t: torch.Tensor) -> Optional[int]:
+    """Elements from row to row of a tensor whose last dimension is a row (0: contiguous); None if that is not one number."""
     if t.is_contiguous():
         return 0
-    if t.dim() == 2 and (t.shape[1] == 1 or t.stride(1) == 1) and (t.shape[0] == 1 or t.stride(0) >= t.shape[1]):
-        return t.stride(0) if t.shape[0] > 1 else 0
-    raise ValueError(f"{what}: strides {tuple(t.stride())} of shape {tuple(t.shape)}: rows of one pitch are needed")
+    *counts, width = t.shape
+    *steps, step = t.stride()
+    if width != 1 and step != 1:
+        return None
+    pitch, rows = None, 1
+    for n, s in zip(reversed(counts), reversed(steps)):
+        if n == 1:
+            continue
+        if pitch is None:
+            pitch = s
+        elif s != pitch * rows:
+            return None
+        rows *= n
+    if pitch is None:
+        return 0
+    return pitch if pitch >= width else None
+
+
+def _pitch(t: torch.Tensor, what: str) -> int:
+    """_pitch_of, where there has to be one."""
+    pitch = _pitch_of(t)
+    if pitch is None:
+        raise ValueError(f"{what}: strides {tuple(t.stride())} of shape {tuple(t.shape)}: rows of one pitch are needed")
+    return pitch
 
 
 def _rows_or_copy(t: torch.Tensor) -> torch.Tensor:
     """t, or its rows one behind another where they have no one pitch."""
-    if t.is_contiguous() or (t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]):
-        return t
-    return t.contiguous()
+    return t if _pitch_of(t) is not None else t.contiguous()
+
+
+def _norm_rows(x: torch.Tensor) -> Tuple[torch.Tensor, int]:
+    """x as layer norm reads it, and its pitch: rows of more than two dimensions that have no one pitch (a slice of a batch) are
+    copied."""
+    if x.is_contiguous():
+        return x, 0
+    if x.dim() > 2 and x.stride(-1) == 1:
+        x = _rows_or_copy(x)
+    return x, _pitch(x, "x")
 
 
 def _rows(t: torch.Tensor, flip: bool):
@@ -463,14 +492,15 @@ def _address(t: torch.Tensor):
 def layer_norm(x: torch.Tensor, gain: torch.Tensor, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
                rms: bool = False, out: Optional[torch.Tensor] = None):
     """fira_layer_norm over the last dimension: (y, mean, rstd); rms: the form without mean and bias (mean is None).  mean
-    and rstd are float32 of x's other dimensions, for layer_norm_grad.  out: may be x itself."""
+    and rstd are float32 of x's other dimensions, for layer_norm_grad.  x's rows have one pitch, or more than two dimensions (a
+    slice of a batch: copied where its rows have no one pitch).  out: may be x itself, where that has one pitch."""
     code = _code(x, "x")
     shape = x.shape
     hidden = shape[-1] if shape else 0
     if hidden == 0:
         raise ValueError(f"x has no rows: {tuple(shape)}")
     params = _check_params(hidden, gain, bias, "gain and bias")
-    ld = 0 if x.is_contiguous() else _pitch(x, "x")
+    x, ld = _norm_rows(x)
     index = _device_of(x, gain, bias, out)
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):
@@ -506,7 +536,7 @@ def layer_norm_grad(dY: torch.Tensor, x: torch.Tensor, gain: torch.Tensor, mean:
     if accumulate and (dgain is None or (dbias is None and not rms)):
         raise ValueError("accumulate: dgain and dbias are needed")
     _check_work(work)
-    ld = 0 if x.is_contiguous() else _pitch(x, "x")
+    x, ld = _norm_rows(x)
     index = _device_of(x, dY, gain, mean, rstd, out, dgain, dbias, work)
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):
