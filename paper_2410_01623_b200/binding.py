@@ -11,6 +11,7 @@ import ctypes as C
 import importlib
 import os
 import sysconfig
+import warnings
 from array import array
 from typing import Optional, Sequence, Tuple
 
@@ -186,6 +187,11 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
 
 def _refuse(what: str):
     raise ValueError(what)
+
+
+def _not_recorded(name: str) -> None:
+    warnings.warn(f"{name} is not recorded for autograd: no gradient reaches its inputs by backward(), call {name}_grad (under "
+                  "torch.no_grad() this is not said)", stacklevel=3)
 
 
 def _code(t: torch.Tensor, what: str) -> int:
@@ -398,7 +404,10 @@ def clip_grads(Gs: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequen
 
 def embedding(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0,
               out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """fira_embedding: scale * table[tokens] (shape of tokens + (hidden,)); zeros where a token is not in 0 .. vocab-1."""
+    """fira_embedding: scale * table[tokens] (shape of tokens + (hidden,)); zeros where a token is not in 0 .. vocab-1.
+    out must not overlap the table.  Not recorded for autograd: the gradient is embedding_grad's."""
+    if table.requires_grad and torch.is_grad_enabled():
+        _not_recorded("embedding")
     code = _code(table, "table")
     bits = _TOKEN_BITS.get(tokens.dtype) or _refuse(f"tokens are int32 or int64, not {tokens.dtype}")
     if table.ndim != 2 or table.numel() == 0:
@@ -493,7 +502,10 @@ def layer_norm(x: torch.Tensor, gain: torch.Tensor, bias: Optional[torch.Tensor]
                rms: bool = False, out: Optional[torch.Tensor] = None):
     """fira_layer_norm over the last dimension: (y, mean, rstd); rms: the form without mean and bias (mean is None).  mean
     and rstd are float32 of x's other dimensions, for layer_norm_grad.  x's rows have one pitch, or more than two dimensions (a
-    slice of a batch: copied where its rows have no one pitch).  out: may be x itself, where that has one pitch."""
+    slice of a batch: copied where its rows have no one pitch).  out: may be x itself, where that has one pitch, and overlaps
+    it in no other way.  Not recorded for autograd: the gradients are layer_norm_grad's."""
+    if (x.requires_grad or gain.requires_grad or (bias is not None and bias.requires_grad)) and torch.is_grad_enabled():
+        _not_recorded("layer_norm")
     code = _code(x, "x")
     shape = x.shape
     hidden = shape[-1] if shape else 0
