@@ -379,8 +379,9 @@ def grad_norm(Gs: Sequence[torch.Tensor], work: Optional[torch.Tensor] = None) -
 def clip_grads(Gs: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None,
                work: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """fira_clip_grads: scales a list of gradients so that their global norm is at most max_norm, in place or into `out`
-    (tensors of the same shapes, float32 or bfloat16 each), and returns the norm before it and the factor, as float32
-    tensors of one element on the device.  work: as for grad_norm."""
+    (tensors of the same shapes, float32 or bfloat16 each, which overlap no gradient but their own, and that from its first
+    element on), and returns the norm before it and the factor, as float32 tensors of one element on the device.  work: as
+    for grad_norm."""
     if out is not None and len(out) != len(Gs):
         raise ValueError(f"{len(out)} outputs for {len(Gs)} gradients")
     _check_work(work)

@@ -371,7 +371,7 @@ fira_status check_list(const char* who, int32_t count, const fira_grad_desc* des
   return FIRA_OK;
 }
 
-// No tensor may be written twice, and one written over its own input keeps its type and layout.
+// No tensor may be written twice or over another one's input, and one written over its own keeps its type and layout.
 fira_status check_outputs(int32_t count, const fira_grad_desc* descs, const void* const* G_dev, void* const* out_dev) {
   if (count <= 0 || !descs || !G_dev) return FIRA_OK;      // said by check_list
   std::vector<const void*> written;
@@ -387,6 +387,13 @@ fira_status check_outputs(int32_t count, const fira_grad_desc* descs, const void
   std::sort(written.begin(), written.end());
   if (std::adjacent_find(written.begin(), written.end()) != written.end()) {
     set_error("fira_clip_grads: a tensor is written twice"); return FIRA_ERR_INVALID_ARG;
+  }
+  for (int i = 0; out_dev && i < count; ++i) {
+    const void* g = G_dev[i];
+    if (descs[i].rows <= 0 || descs[i].cols <= 0 || out_dev[i] == g || g < written.front() || g > written.back()) continue;
+    if (std::binary_search(written.begin(), written.end(), g)) {
+      set_error("fira_clip_grads: tensor " + std::to_string(i) + " is the output of another one"); return FIRA_ERR_INVALID_ARG;
+    }
   }
   return FIRA_OK;
 }
