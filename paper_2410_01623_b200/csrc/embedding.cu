@@ -36,10 +36,9 @@ __device__ __forceinline__ int token_at(const TOK* tokens, long long i, int voca
 }
 
 // Wide rows of whole 16-byte units on 16-byte boundaries: a warp takes LK_ROWS positions and a slice of 32 units.
-// (131072 rows of 1024, bf16: 55 us; by k_embedding_words 64.  Of 64, fp32: 10.3 and 9.7.)  Eight blocks to an SM: 65536 rows of 1024, bf16, 36.4 us;
-// with the 34 registers that the compiler takes otherwise, 37.2.
+// (131072 rows of 1024, bf16: 55 us; by k_embedding_words 64.  Of 64, fp32: 10.3 and 9.7.)
 template <typename T, typename TOK>
-__global__ void __launch_bounds__(EM_THREADS, 8)
+__global__ void __launch_bounds__(EM_THREADS)
 k_embedding_rows(const T* __restrict__ table, long long ld, const TOK* __restrict__ tokens, long long n, int vocab, int hidden, int slices,
                  float scale, T* __restrict__ out, long long ld_out) {
   constexpr int N = rows::PER16<T>;
@@ -56,11 +55,10 @@ k_embedding_rows(const T* __restrict__ table, long long ld, const TOK* __restric
 #pragma unroll
   for (int u = 0; u < LK_ROWS; ++u) {
     if (i0 + u >= n) break;
-    const float by = t[u] >= 0 ? scale : 0.f;          // (a row of zeros whatever the factor)
     float2 v[N / 2];
     rows::unpack<T>(a[u], v);
 #pragma unroll
-    for (int e = 0; e < N / 2; ++e) v[e] = rows::mul2(v[e], rows::both(by));
+    for (int e = 0; e < N / 2; ++e) v[e] = rows::mul2(v[e], rows::both(scale));
     *reinterpret_cast<uint4*>(out + (i0 + u) * ld_out + col) = rows::pack<T>(v);
   }
 }
@@ -69,6 +67,8 @@ k_embedding_rows(const T* __restrict__ table, long long ld, const TOK* __restric
 // own, so that rows of any width keep all lanes busy.  ALIGNED (one word, two items of a thread): all rows are whole
 // 16-byte units on 16-byte boundaries.  Otherwise (two words, one item) they are funnelled from three aligned words of the table,
 // of which those are read that hold a byte of them (131072 rows of 1023, bf16: 83 us; one word and two items 103).
+// Factors that are not finite, or negative, go that way too, wherever the rows begin: there alone a position without a token has a factor of
+// its own, 0, since its zeros are multiplied like the rest (that factor in all kernels: 131072 rows of 1024, bf16, 54.0 -> 54.9 us; 200000 of 64, 9.7 -> 10.5).
 template <bool ALIGNED>
 constexpr int LK_WORDS = ALIGNED ? 1 : 2;
 template <bool ALIGNED>
@@ -84,7 +84,7 @@ k_embedding_words(const T* __restrict__ table, long long ld, const TOK* __restri
   uint4 a[LK_EACH][W + (ALIGNED ? 0 : 1)];
   T* to[LK_EACH];                           // the first word, and the column of its first element (hidden: none)
   int col[LK_EACH], skip[LK_EACH];
-  bool none[LK_EACH];                       // no token: a row of zeros, whatever the factor
+  bool none[LK_EACH];                       // no token
 #pragma unroll
   for (int u = 0; u < LK_EACH; ++u) {
     const unsigned x = item0 + u * EM_THREADS + threadIdx.x, down = x / items;      // (items < 2^23: no overflow)
@@ -120,7 +120,7 @@ k_embedding_words(const T* __restrict__ table, long long ld, const TOK* __restri
       uint4 x = a[u][w];
       if constexpr (!ALIGNED) x = rows::funnel16(a[u][w], a[u][w + 1], skip[u]);
       if (scale != 1.f) {
-        const float by = none[u] ? 0.f : scale;
+        const float by = !ALIGNED && none[u] ? 0.f : scale;
         float2 v[N / 2];
         rows::unpack<T>(x, v);
 #pragma unroll
@@ -774,7 +774,7 @@ unsigned words_of(long long hidden, size_t size, bool aligned) { return (unsigne
 template <typename T, typename TOK>
 void run_lookup(const void* table, long long ld, const void* tokens, long long n, int vocab, int hidden, float scale, void* out, long long ld_out,
                 cudaStream_t st) {
-  const bool aligned = rows::aligned16(table, ld, hidden, sizeof(T)) && rows::aligned16(out, ld_out, hidden, sizeof(T));
+  const bool aligned = rows::aligned16(table, ld, hidden, sizeof(T)) && rows::aligned16(out, ld_out, hidden, sizeof(T)) && isfinite(scale) && !signbit(scale);
   const unsigned words = words_of(hidden, sizeof(T), aligned), items = aligned ? words : (words + LK_WORDS<false> - 1) / LK_WORDS<false>;
   const int per_block = EM_THREADS * (aligned ? LK_ITEMS<true> : LK_ITEMS<false>);
   const unsigned blocks = (unsigned)((n * items + per_block - 1) / per_block);
