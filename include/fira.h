@@ -195,9 +195,12 @@ typedef struct {
 /* G_dev: a host array of `count` device pointers, aligned to their elements (rows that start on 16-byte boundaries are
  * the fast case).  out_dev = NULL: in place, and nothing is written where s = 1; otherwise an array like G_dev: out_i is G_i
  * itself (same type and ld) or overlaps no tensor of the list, and no tensor is written twice.  The norm goes to
- * norm_dev[0] and s to scale_dev[0] (device floats).  Squares are added up in double over the whole range of the
- * types, in the same order in every call.  Where N is not finite (an infinity or a NaN among the gradients) s is 1: the
- * gradients are passed on as they are and N tells.  max_norm > 0 (+inf: never clipped).
+ * norm_dev[0] and s to scale_dev[0] (device floats).  32 squares at a time are added up in fp32, or in double where their sum leaves
+ * the range in which that loses nothing but roundings, and these sums in double: N holds over the whole range of the types, to 17 2^-24
+ * of itself.  The same call adds in the same order; which elements are added together first depends on how the tensors (and, in
+ * fira_clip_grads(), the outputs) lie to 16-byte boundaries, so other buffers may change N's last bit.  Where N is not finite (an
+ * infinity or a NaN among the gradients) s is 1: the gradients are passed on as they are and N tells.  (A finite N above the floats' range
+ * is stored as an infinity, beside an s that is max_norm / N.)  max_norm > 0 (+inf: never clipped).
  * work_dev: 16-byte aligned, fira_grad_work_bytes(count) bytes, of one call at a time; its contents need not be kept or
  * set.  Needs no context.  Asynchronous on cuda_stream. */
 FIRA_API size_t fira_grad_work_bytes(int32_t count);
@@ -213,9 +216,9 @@ FIRA_API fira_status fira_clip_grads(int32_t count, const fira_grad_desc* descs,
  * in 0 .. vocab-1 (-1 behind the end of a sequence) gives a row of zeros and has no part in the gradient.  Rows have
  * `hidden` elements and are ld (ld_out, ldg) elements apart (0: hidden); tensors are aligned to their elements, and rows of
  * whole 16-byte units that start on 16-byte boundaries are the fast case.  Products and sums are fp32 and rounded once; the
- * order of a sum depends on the tokens alone, so the same call gives the same bits.
+ * order of a sum depends on the tokens and sizes alone, so the same call gives the same bits.
  * Lookup: table and out have type dtype; out must not overlap the table.
- * Gradient: dY has type dtype, G (vocab rows) type grad_dtype.  accumulate = 0: all of G is written, rows without a token
+ * Gradient: dY has type dtype, G (vocab rows) type grad_dtype, and overlaps neither dY nor the tokens.  accumulate = 0: all of G is written, rows without a token
  * as zeros.  accumulate != 0: the sums are added to what is there (micro-batches; a table that is also the output head),
  * and rows without a token are left alone.  work_dev: 256-byte aligned, fira_embedding_grad_work_bytes() bytes of the same
  * sizes (0: sizes that the call refuses), of one call at a time; its contents need not be kept or set.
@@ -239,8 +242,8 @@ FIRA_API fira_status fira_embedding_grad(const void* tokens_dev, int32_t token_b
  * x, y, dY, dX have type dtype and rows ld elements apart (0: hidden); gain and bias type param_dtype; dgain and dbias type
  * grad_dtype.  bias_dev may be NULL (none), dbias_dev too (not wanted).  Tensors are aligned to their elements; rows of whole 16-byte units that
  * start on 16-byte boundaries are the fast case.  The forward pass writes rstd_dev[row] = s and mean_dev[row] = mu, which
- * the backward pass takes.  Arithmetic and sums are fp32, rounded once; the sums over rows are made in the same order in
- * every call.  accumulate != 0: dgain and dbias are added to what is there.
+ * the backward pass takes.  Arithmetic and sums are fp32, rounded once; the same call adds in the same order (which depends on the sizes and on
+ * how the rows lie to 16-byte boundaries).  accumulate != 0: dgain and dbias are added to what is there.
  * y may be x itself, dX may be dY or x itself (same ld); otherwise they overlap nothing.  nrows = 0 is allowed (dgain and dbias
  * are then zero, or left as they are).  work_dev: 256-byte aligned, fira_layer_norm_grad_work_bytes() bytes of the same
  * sizes (0: sizes that the call refuses), of one call at a time; its contents need not be kept or set.  Rows are read in

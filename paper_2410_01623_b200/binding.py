@@ -254,8 +254,6 @@ def _rows_or_copy(t: torch.Tensor) -> torch.Tensor:
 def _norm_rows(x: torch.Tensor) -> Tuple[torch.Tensor, int]:
     """x as layer norm reads it, and its pitch: rows of more than two dimensions that have no one pitch (a slice of a batch) are
     copied."""
-    if x.is_contiguous():
-        return x, 0
     if x.dim() > 2 and x.stride(-1) == 1:
         x = _rows_or_copy(x)
     return x, _pitch(x, "x")
@@ -306,7 +304,7 @@ def _native_grad_list(Gs, out):
     try:
         module = importlib.import_module("._native_lists", __package__)
         fits = (module.torch_version, module.desc_bytes) == (torch.__version__, C.sizeof(GradDesc))
-    except (ImportError, AttributeError):
+    except (ImportError, AttributeError, TypeError):     # (TypeError: this file on its own, in no package)
         fits = False
     _native_grad_list = module.grad_list if fits else lambda Gs, out: None
     return _native_grad_list(Gs, out)
@@ -438,7 +436,7 @@ def embedding_grad(tokens: torch.Tensor, dY: torch.Tensor, vocab: int, scale: fl
                    out: Optional[torch.Tensor] = None, accumulate: bool = False,
                    work: Optional[torch.Tensor] = None) -> torch.Tensor:
     """fira_embedding_grad: the gradient (vocab, hidden) of the table from that of scale * table[tokens].  out: float32 or
-    bfloat16, by default a new tensor of dY's type; accumulate: added to what is in it.  work: a byte tensor of at least
+    bfloat16, by default a new tensor of dY's type, and no part of dY; accumulate: added to what is in it.  work: a byte tensor of at least
     lib().fira_embedding_grad_work_bytes() bytes; by default torch's allocator lends one for the call."""
     code = _code(dY, "dY")
     bits = _TOKEN_BITS.get(tokens.dtype) or _refuse(f"tokens are int32 or int64, not {tokens.dtype}")
@@ -513,7 +511,7 @@ def layer_norm(x: torch.Tensor, gain: torch.Tensor, bias: Optional[torch.Tensor]
     if hidden == 0:
         raise ValueError(f"x has no rows: {tuple(shape)}")
     params = _check_params(hidden, gain, bias, "gain and bias")
-    x, ld = _norm_rows(x)
+    x, ld = (x, 0) if x.is_contiguous() else _norm_rows(x)
     index = _device_of(x, gain, bias, out)
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):
@@ -549,7 +547,7 @@ def layer_norm_grad(dY: torch.Tensor, x: torch.Tensor, gain: torch.Tensor, mean:
     if accumulate and (dgain is None or (dbias is None and not rms)):
         raise ValueError("accumulate: dgain and dbias are needed")
     _check_work(work)
-    x, ld = _norm_rows(x)
+    x, ld = (x, 0) if x.is_contiguous() else _norm_rows(x)
     index = _device_of(x, dY, gain, mean, rstd, out, dgain, dbias, work)
     if index != torch.cuda.current_device():
         with torch.cuda.device(index):

@@ -3,7 +3,8 @@
 //   Y_i = a E[t_i]                         (t_i outside 0 .. vocab-1: a row of zeros)
 //   dE_v = a sum over {i : t_i = v} of dY_i
 //
-// The gradient takes two launches.  k_token_order groups the positions by token: each block owns the tokens of one
+// The gradient takes two launches, or three for large batches (k_token_split and k_token_gather in place of k_token_order, each token
+// read once).  k_token_order groups the positions by token: each block owns the tokens of one
 // remainder by the number of blocks (so that the frequent ones, which in most vocabularies lie side by side, fall to different blocks)
 // and reads all tokens of the batch, which stay in L2.  It counts those of lower remainders, which is where its own
 // positions begin, and lists its own in shared memory; then it sorts the list by row.  No block waits for another, and the

@@ -4,8 +4,8 @@
 //
 // Two kernels over a list of tensors whose table travels in the kernel arguments (nothing is allocated, nothing of
 // it outlives the call).  k_grad_squares leaves one sum of squares per block; k_grad_scale adds those up in a fixed
-// order in every block (they are a few KB), so that no third launch lies between, and scales.  Sums are the same in
-// every call: no atomics.
+// order in every block (they are a few KB), so that no third launch lies between, and scales.  The same call gives the same sums: no
+// atomics.  (Which elements are a thread's depends on the tensors' and outputs' places between 16-byte boundaries.)
 //
 // A thread squares 32 elements into one fp32 sum and adds that to a double.  Where the fp32 sum says nothing (it left
 // the range in which neither an overflow nor what underflowed matters) the elements, still in registers, are squared

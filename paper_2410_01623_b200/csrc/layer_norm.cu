@@ -4,8 +4,9 @@
 //   with h = (x - mu) s, q = dy g:   dx = s (q - mean(q) - h mean(q h))   (RMS: without mean(q))
 //   dg = sum over rows of dy h,   db = sum over rows of dy
 //
-// A group of 4 to 1024 threads takes a row, each thread 16 elements of it, which stay in registers (as they were read)
-// from the load to the store; the next row is on its way meanwhile.  Gain and bias lie in shared memory in the order in which
+// A group of 4 to 1024 threads takes a row, each thread 16 elements of it: fetched once, into shared memory, where only this thread
+// reads them (in the backward pass with mean or of more than 8192 columns twice: there are no registers to keep them in); the next rows
+// are on their way meanwhile, where there is room.  Gain and bias lie in shared memory in the order in which
 // the threads read them.  Statistics are fp32, the variance from the differences to the mean.  In the backward pass a
 // thread has the same columns in every row of its group, so that dg and db grow in its registers; the groups of a block are added in shared memory, the
 // blocks in a second launch, always in the same order.
@@ -171,8 +172,8 @@ constexpr int GRAD_STAGES = THREADS == 1024 ? (sizeof(T) == 2 ? 2 : 1) : THREADS
 template <typename T, int THREADS>
 constexpr size_t GRAD_SMEM = (size_t)LN_EACH * sizeof(float) + 2 * GRAD_STAGES<T, THREADS> * LN_EACH * sizeof(T);
 
-// Blocks of the backward pass on an SM (where rows take LN_THREADS threads at most): three where the registers suffice (65536 rows of
-// 512, bf16, without mean: 45 us), two of more registers elsewhere (of 256, fp32: 62 us with three, 43 with two).
+// Blocks of the backward pass on an SM (where rows take LN_THREADS threads at most): three where 80 registers nearly suffice (56 bytes of a
+// thread spilled; 65536 rows of 512, bf16, without mean: 45 us), two of more registers elsewhere (of 256, fp32: 62 us with three, 43 with two).
 template <typename T, Mode MODE, bool RMS, int THREADS>
 constexpr int GRAD_RESIDENT = THREADS > LN_THREADS ? 1 : RMS && MODE == ALIGNED && sizeof(T) == 2 ? 3 : 2;
 
